@@ -272,6 +272,112 @@ dbt_status dbt_decode_step_ungrouped(dbt_model *m, dbt_kv *kv, const dbt_step_in
 dbt_status dbt_decode_step_noalloc(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, int32_t branch_on,
                                    dbt_step_out *out, dbt_stream stream);
 
+/* ---- drafted tokens -----------------------------------------------------
+ * Several guessed next tokens of each sequence evaluated in one pass: a tree
+ * of drafted tokens (nodes) hangs below the cached positions, every node sees
+ * the cache and its own line of ancestors, and afterwards the cache keeps the
+ * accepted path:
+ *   dbt_decode_tree     the grouped step over the nodes; the sequences grow by
+ *                       their nodes, node i at the i-th new position
+ *   dbt_sample          a token after every node (or the readout's greedy one)
+ *   dbt_tree_accept     the line of drafted tokens that agrees with them
+ *   dbt_kv_keep         moves its keys and values together, ends the sequences there
+ * While a sequence ends in nodes that were not kept or dropped
+ * (dbt_kv_truncate), other calls take those positions for ordinary ones. */
+
+/* The drafted nodes of sequences 0..batch-1, sequence after sequence.  A
+ * sequence without nodes takes no part.  parents[i] is the index, among its own
+ * sequence's nodes, of the node that node i follows, or -1 when it follows the
+ * cached positions; it must be smaller than the node's own index (any other
+ * value reads as -1). */
+#define DBT_TREE_NODES 64
+typedef struct {
+  int32_t batch;
+  const int32_t *h_nodes; /* HOST [batch]: nodes per sequence, 0..DBT_TREE_NODES; at least one in all */
+  const int32_t *parents; /* [sum h_nodes] */
+} dbt_tree;
+
+/* Bytes of the workspace (256-byte aligned) that tree calls of a model of this
+ * configuration need for up to `nodes` nodes in all (0 on bad arguments).
+ * Calls that may overlap need workspaces of their own. */
+size_t dbt_tree_workspace_bytes(const dbt_config *cfg, int32_t nodes);
+
+/* Grows every sequence by its nodes (host-only; dbt_decode_tree does it itself). */
+dbt_status dbt_tree_reserve(dbt_kv *kv, const dbt_tree *tree);
+
+/* Attention of drafted nodes over one layer of the cache.  The last h_nodes[b]
+ * positions of sequence b are its nodes, their keys and values already there
+ * (dbt_kv_fill); node i sees every position before them, itself and its
+ * ancestors.  q and out, in the model's dtype: [n_paths][sum h_nodes][n_q][d_h],
+ * paths 1..1 + n_branches as in a step (Eqs. (9), (12)).  The keys and values
+ * that a node does not see leave no trace in its rows, whatever they hold.  The
+ * same call repeats its bits; the number of splits of a long cache follows from
+ * the whole call, so rows can differ by rounding from one batch to another. */
+dbt_status dbt_tree_attention(dbt_kv *kv, int32_t layer, const dbt_tree *tree, int32_t n_paths, const void *q,
+                              void *out, void *workspace, dbt_stream stream);
+
+/* dbt_decode_step over the nodes of a tree: in->batch is sum h_nodes (at most
+ * max_batch), its tokens or residual inputs and every output are per node, and
+ * node i has position len_b + its depth.  The primary appends the nodes' keys and values, the
+ * sequences grow by their nodes. */
+dbt_status dbt_decode_tree(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, const dbt_tree *tree, int32_t branch_on,
+                           dbt_step_out *out, void *workspace, dbt_stream stream);
+
+/* Host-only.  From node 0, which always stays (the token that the last call
+ * answered), the path follows the first child whose drafted token is the one
+ * drawn after the node, as long as there is one.  Every array is host memory and
+ * laid out as dbt_tree: h_tokens are the nodes' own tokens, h_drawn the tokens
+ * drawn after them.  h_path
+ * (room for sum h_nodes) receives the kept nodes' indices, ascending, sequence after sequence;
+ * h_kept[b] is their number, h_next[b] (may be NULL) the token drawn after the last of
+ * them (-1 for a sequence without nodes). */
+dbt_status dbt_tree_accept(int32_t batch, const int32_t *h_nodes, const int32_t *h_parents, const int32_t *h_tokens,
+                           const int32_t *h_drawn, int32_t *h_path, int32_t *h_kept, int32_t *h_next);
+
+/* The last h_nodes[b] positions of each sequence of the tree (parents may be
+ * NULL) are nodes; h_kept[b] of them stay, those with the ascending indices in
+ * h_path [sum h_kept], sequence after sequence.  Their keys and values move, in
+ * every layer, to the first positions of the nodes; the sequence ends behind them and gives
+ * back the pages past its end. */
+dbt_status dbt_kv_keep(dbt_kv *kv, const dbt_tree *tree, const int32_t *h_kept, const int32_t *h_path,
+                       dbt_stream stream);
+
+/* ---- drawn tokens ------------------------------------------------------- */
+
+/* How a row's token is drawn. */
+typedef struct {
+  float temperature; /* >= 0; 0 answers the greedy token */
+  float top_p;       /* (0, 1]; 1 cuts nothing */
+  float min_p;       /* [0, 1]; 0 cuts nothing */
+  int32_t top_k;     /* >= 0; 0 cuts nothing */
+} dbt_sampling;
+
+typedef struct {
+  const float *logits1;  /* [rows][vocab] primary logits */
+  const float *logits2;  /* [n_branches][rows][vocab] branch logits; unused without branches */
+  const float *alpha;    /* [rows] mixture weights (dbt_step_out.alpha), in [0, 1]; unused without branches */
+  const float *u;        /* [rows] random numbers in [0, 1) */
+  const dbt_sampling *h_params; /* HOST [rows] */
+  int32_t rows, vocab;
+  int32_t n_branches;    /* 0..3; 0: the primary's distribution alone */
+} dbt_sample_in;
+
+size_t dbt_sample_workspace_bytes(int32_t rows, int32_t vocab);
+
+/* One token per row from the mixture m = alpha p + (1 - alpha) q of the readout
+ * (Sec. 4.2, Eqs. (17)-(18); q the mean of the branches).  Token v weighs
+ * w_v = (m_v / max m)^(1 / temperature).  In the order of falling weight, equal
+ * ones by index, the first top_k tokens stay, of them the shortest run whose sum
+ * reaches top_p of theirs, of that those with w_v >= min_p; the row's token is the
+ * lowest index at which the running sum of the weights that stayed exceeds u
+ * times their sum.  prob (may be NULL) [rows]: its share of that sum.  Weights are
+ * evaluated in float64 and held as multiples of 2^-42 or a finer step, so that
+ * every sum is exact and a row's token depends on nothing but its row.  A row that holds a NaN or +infinity, nothing
+ * above -infinity, or an alpha outside [0, 1] gets token -1 and probability 0; u below
+ * 0 (or NaN) reads as 0, u of 1 or more as the largest below 1.  Needs no model.
+ * rows at most 65535, vocab at most 2^20. */
+dbt_status dbt_sample(const dbt_sample_in *in, int32_t *token, float *prob, void *workspace, dbt_stream stream);
+
 /* ---- stage timing -------------------------------------------------------
  * While enabled for a stage, every later device call records a HIP event pair
  * on its stream around the kernel(s) of that stage, once per launch.

@@ -58,6 +58,19 @@ class dbt_step_out(ctypes.Structure):
                                  "route_logits1", "route_logits2")]
 
 
+class dbt_tree(ctypes.Structure):
+    _fields_ = [("batch", I32), ("h_nodes", ctypes.POINTER(I32)), ("parents", P)]
+
+
+class dbt_sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float), ("top_k", I32)]
+
+
+class dbt_sample_in(ctypes.Structure):
+    _fields_ = [("logits1", P), ("logits2", P), ("alpha", P), ("u", P), ("h_params", ctypes.POINTER(dbt_sampling)),
+                ("rows", I32), ("vocab", I32), ("n_branches", I32)]
+
+
 _lib = None
 
 _SIGS = {
@@ -78,6 +91,15 @@ _SIGS = {
     "dbt_decode_step": (I32, [P, P, ctypes.POINTER(dbt_step_in), I32, ctypes.POINTER(dbt_step_out), P]),
     "dbt_decode_step_ungrouped": (I32, [P, P, ctypes.POINTER(dbt_step_in), ctypes.POINTER(dbt_step_out), P]),
     "dbt_decode_step_noalloc": (I32, [P, P, ctypes.POINTER(dbt_step_in), I32, ctypes.POINTER(dbt_step_out), P]),
+    "dbt_tree_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(dbt_config), I32]),
+    "dbt_tree_reserve": (I32, [P, ctypes.POINTER(dbt_tree)]),
+    "dbt_tree_attention": (I32, [P, I32, ctypes.POINTER(dbt_tree), I32, P, P, P, P]),
+    "dbt_decode_tree": (I32, [P, P, ctypes.POINTER(dbt_step_in), ctypes.POINTER(dbt_tree), I32,
+                              ctypes.POINTER(dbt_step_out), P, P]),
+    "dbt_tree_accept": (I32, [I32] + [ctypes.POINTER(I32)] * 7),
+    "dbt_kv_keep": (I32, [P, ctypes.POINTER(dbt_tree), ctypes.POINTER(I32), ctypes.POINTER(I32), P]),
+    "dbt_sample_workspace_bytes": (ctypes.c_size_t, [I32, I32]),
+    "dbt_sample": (I32, [ctypes.POINTER(dbt_sample_in), P, P, P, P]),
     "dbt_stage_timing": (I32, [P, I32, I32]),
     "dbt_stage_time": (ctypes.c_double, [P, I32, ctypes.POINTER(I32)]),
 }
@@ -190,6 +212,72 @@ def dbt_decode_step_ungrouped(m, kv, step_in, out, stream):
 
 def dbt_decode_step_noalloc(m, kv, step_in, branch_on, out, stream):
     _check(lib().dbt_decode_step_noalloc(m, kv, ctypes.byref(step_in), branch_on, ctypes.byref(out), P(stream)))
+
+
+def _ints(values):
+    return (I32 * max(1, len(values)))(*values)
+
+
+def make_tree(nodes, parents_ptr=None):
+    """A dbt_tree of `nodes[b]` drafted nodes per sequence, parents in device memory."""
+    return dbt_tree(batch=len(nodes), h_nodes=_ints([int(n) for n in nodes]), parents=parents_ptr)
+
+
+def make_paths(paths):
+    """Kept nodes per sequence (lists of ascending indices) as dbt_kv_keep takes
+    them: their numbers and the indices one after another."""
+    return _ints([len(p) for p in paths]), _ints([int(i) for p in paths for i in p]), len(paths)
+
+
+def make_sampling(params):
+    """Host array of dbt_sampling from (temperature, top_k, top_p, min_p) per row."""
+    return (dbt_sampling * len(params))(*[dbt_sampling(temperature=t, top_k=k, top_p=p, min_p=mp)
+                                          for t, k, p, mp in params])
+
+
+def dbt_tree_workspace_bytes(cfg, nodes):
+    return lib().dbt_tree_workspace_bytes(ctypes.byref(cfg), nodes)
+
+
+def dbt_tree_reserve(kv, tree):
+    _check(lib().dbt_tree_reserve(kv, ctypes.byref(tree)))
+
+
+def dbt_tree_attention(kv, layer, tree, n_paths, q_ptr, out_ptr, workspace_ptr, stream):
+    _check(lib().dbt_tree_attention(kv, layer, ctypes.byref(tree), n_paths, P(q_ptr), P(out_ptr), P(workspace_ptr),
+                                    P(stream)))
+
+
+def dbt_decode_tree(m, kv, step_in, tree, branch_on, out, workspace_ptr, stream):
+    _check(lib().dbt_decode_tree(m, kv, ctypes.byref(step_in), ctypes.byref(tree), branch_on, ctypes.byref(out),
+                                 P(workspace_ptr), P(stream)))
+
+
+def dbt_tree_accept(nodes, parents, tokens, drawn):
+    """Kept nodes of each sequence and the token drawn after the last of them (host data)."""
+    n = sum(nodes)
+    if not len(parents) == len(tokens) == len(drawn) == n:
+        raise ValueError("parents, tokens and drawn need one entry per node")
+    path, kept, nxt = _ints([0] * n), _ints([0] * len(nodes)), _ints([0] * len(nodes))
+    _check(lib().dbt_tree_accept(len(nodes), _ints(nodes), _ints(parents), _ints(tokens), _ints(drawn), path, kept, nxt))
+    end = np.cumsum([0] + list(kept)[:len(nodes)])
+    return [path[end[b]:end[b + 1]] for b in range(len(nodes))], list(nxt)[:len(nodes)]
+
+
+def dbt_kv_keep(kv, tree, paths, stream):
+    """Keeps the nodes of make_paths (one list per sequence of the tree)."""
+    kept, path, batch = paths
+    if batch != tree.batch:
+        raise ValueError("one list of kept nodes per sequence of the tree")
+    _check(lib().dbt_kv_keep(kv, ctypes.byref(tree), kept, path, P(stream)))
+
+
+def dbt_sample_workspace_bytes(rows, vocab):
+    return lib().dbt_sample_workspace_bytes(rows, vocab)
+
+
+def dbt_sample(sample_in, token_ptr, prob_ptr, workspace_ptr, stream):
+    _check(lib().dbt_sample(ctypes.byref(sample_in), P(token_ptr), P(prob_ptr), P(workspace_ptr), P(stream)))
 
 
 def dbt_stage_timing(m, stage, enable):
@@ -362,6 +450,49 @@ class Session:
                     int(run_boundary), out, self.stream)
         torch.cuda.current_stream().synchronize()
         return t
+
+    def decode_tree(self, nodes, parents, tokens=None, h1=None, h2=None, branch_on=True, logits=True):
+        """The step over drafted nodes (dbt_decode_tree): nodes[b] per sequence,
+        parents and tokens (or residual inputs) one entry per node."""
+        torch = self.torch
+        n = int(sum(nodes))
+        up = torch.as_tensor(np.asarray(parents, np.int32)).to(self.device)
+        tk = None if tokens is None else torch.as_tensor(np.asarray(tokens, np.int32)).to(self.device)
+        h1d = None if h1 is None else torch.as_tensor(np.ascontiguousarray(h1, np.float32)).to(self.device)
+        h2d = None if h2 is None else torch.as_tensor(np.ascontiguousarray(h2, np.float32)).to(self.device)
+        sizes = [up.numel()] + ([tk.numel()] if tk is not None else [h1d.shape[0]] if h1d is not None else [])
+        if any(x != n for x in sizes):
+            raise ValueError("parents and inputs need one entry per node")
+        ws = torch.empty(dbt_tree_workspace_bytes(self.cfg, max(1, n)), dtype=torch.uint8, device=self.device)
+        out, t = self.outputs(n, logits=logits, routing=True)
+        dbt_decode_tree(self.model, self.kv, self.step_in(n, tk, h1d, h2d), make_tree(nodes, up.data_ptr()),
+                        int(branch_on), out, ws.data_ptr(), self.stream)
+        torch.cuda.current_stream().synchronize()
+        return t
+
+    def sample(self, t, u, params, branch_on=True):
+        """Tokens and their probabilities drawn from the outputs `t` of a step
+        (decode, decode_tree or prefill, with logits): u and params, a
+        (temperature, top_k, top_p, min_p), per row."""
+        torch = self.torch
+        rows, vocab = t["logits1"].shape
+        ud = torch.as_tensor(np.asarray(u, np.float32)).to(self.device)
+        if ud.numel() != rows or len(params) != rows:
+            raise ValueError("u and params need one entry per row")
+        token = torch.empty(rows, dtype=torch.int32, device=self.device)
+        prob = torch.empty(rows, dtype=torch.float32, device=self.device)
+        ws = torch.empty(dbt_sample_workspace_bytes(rows, vocab), dtype=torch.uint8, device=self.device)
+        sin = dbt_sample_in(logits1=_ptr(t["logits1"]), logits2=_ptr(t["logits2"]) if branch_on else None,
+                            alpha=_ptr(t["alpha"]) if branch_on else None, u=_ptr(ud), h_params=make_sampling(params),
+                            rows=rows, vocab=vocab, n_branches=self.n_branches if branch_on else 0)
+        dbt_sample(sin, token.data_ptr(), prob.data_ptr(), ws.data_ptr(), self.stream)
+        torch.cuda.current_stream().synchronize()
+        return token, prob
+
+    def keep(self, nodes, paths):
+        """Ends every sequence after the kept ones of its last nodes[b] positions (dbt_kv_keep)."""
+        dbt_kv_keep(self.kv, make_tree(nodes), make_paths(paths), self.stream)
+        self.torch.cuda.current_stream().synchronize()
 
     def decode(self, tokens=None, h1=None, h2=None, branch_on=True, grouped=True, batch=None, logits=True):
         torch = self.torch

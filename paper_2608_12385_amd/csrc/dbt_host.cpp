@@ -484,6 +484,16 @@ dbt_status flush(dbt_kv *kv, const int *h_pos, int npos, hipStream_t st, StepBeg
   return DBT_OK;
 }
 
+// A tree call's sequences in launches of up to kTreeSeqs, how its attention
+// splits the cache, and its workspace.
+struct TreePlan {
+  std::vector<TreeSeqs> groups;
+  const int *parents = nullptr;
+  int nodes = 0, max_nodes = 0, pages_per_split = 1, max_splits = 1;
+  float *opart = nullptr, *ostat = nullptr;
+  PromptRow *map = nullptr;
+};
+
 // One layer for the active rows.  rows_layout: rows of the partial slabs.
 struct LayerCall {
   Rows rows;
@@ -499,7 +509,22 @@ struct LayerCall {
   const HIn *hin;
   const StepBegin *sb;
   HOut ho;  // where the last layer leaves the states (see HOut)
+  const TreePlan *tree;  // the rows are drafted nodes (NULL: one row per sequence)
 };
+
+hipError_t tree_attn(const TreePlan &t, TreeAttn a, hipStream_t st) {
+  a.parents = t.parents;
+  a.pages_per_split = t.pages_per_split;
+  a.max_splits = t.max_splits;
+  a.max_nodes = t.max_nodes;
+  a.opart = t.opart;
+  a.ostat = t.ostat;
+  for (const TreeSeqs &s : t.groups) {
+    a.s = s;
+    if (const hipError_t e = launch_tree_attn(a, st)) return e;
+  }
+  return hipSuccess;
+}
 
 // Whether the decode attention of B sequences, the longest of maxlen positions
 // after the append, reads each (sequence, KV head) in one workgroup: bf16 where
@@ -781,7 +806,7 @@ dbt_status run_moe_mlp(dbt_model *m, int l, const LayerCall &c, hipStream_t st) 
 dbt_status run_layer(dbt_model *m, dbt_kv *kv, int l, const LayerCall &c, hipStream_t st) {
   const dbt_config &cf = m->cfg;
   const Layout &L = c.prefill ? m->Lp : m->L;
-  const PromptRow *map = c.prefill ? m->at<PromptRow>(L.prow) : nullptr;
+  const PromptRow *map = c.prefill ? m->at<PromptRow>(L.prow) : c.tree ? c.tree->map : nullptr;
   const dbt_layer_weights &W = m->layers[l];
   const int d = cf.d_model, dq = cf.n_q_heads * cf.head_dim, dkv = cf.n_kv_heads * cf.head_dim, f = L.f;
   const size_t es = esize(cf);
@@ -878,9 +903,9 @@ dbt_status run_layer(dbt_model *m, dbt_kv *kv, int l, const LayerCall &c, hipStr
   // Decode on the bf16 cache: the attention kernel finishes the queries and
   // appends the cache entry itself.
   int maxlen = 0;
-  if (!c.prefill)
+  if (!c.prefill && !c.tree)
     for (int b = 0; b < c.rows.B; ++b) maxlen = std::max(maxlen, kv->len[b] + 1);  // (the boundary: one too many)
-  const bool finish_in_attn = !c.prefill && cf.dtype == DBT_BF16;
+  const bool finish_in_attn = !c.prefill && !c.tree && cf.dtype == DBT_BF16;
   const bool xin = l == 0 && c.hin && c.hin->h1;
   if (xin && (c.prefill || !finish_in_attn || cf.dtype != DBT_BF16 || !gemm_xnorm_ok(g_qkv, aM)))
     return fail(DBT_ERR_STATE, "internal: first-layer input fold on an unsupported call");
@@ -917,7 +942,7 @@ dbt_status run_layer(dbt_model *m, dbt_kv *kv, int l, const LayerCall &c, hipStr
   qf.rows = arows;
   qf.mode = amode;
   qf.rope = m->at<float2>(L.rope);
-  qf.pos_arr = c.prefill ? nullptr : m->at<int>(L.pos);
+  qf.pos_arr = map ? nullptr : m->at<int>(L.pos);
   qf.prompt = map;
   qf.a = W.a;
   qf.Q = Q;
@@ -945,6 +970,18 @@ dbt_status run_layer(dbt_model *m, dbt_kv *kv, int l, const LayerCall &c, hipStr
     pa.O = O;
     pa.ldo = dq;
     HIPCHK(launch_attn_prefill(pa, st));
+  } else if (c.tree) {
+    TreeAttn ta{};
+    ta.Q = Q;
+    ta.q32 = true;
+    ta.O = O;
+    ta.path_rows = arows.Bp;
+    ta.kv = kvl;
+    ta.n_q = cf.n_q_heads;
+    ta.np = arows.np;
+    ta.dtype = cf.dtype;
+    Timed tm(m, DBT_STAGE_ATTN, st);
+    HIPCHK(tree_attn(*c.tree, ta, st));
   } else {
     AttnArgs aa{};
     aa.Q = Q;
@@ -1326,6 +1363,131 @@ dbt_status decode_step_impl(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, int
   return step_done(kv, B);
 }
 
+// ---- drafted tokens ----
+
+// Pages a tree's attention reads per workgroup: at least kTreeMinPages, the
+// most the kernel holds page ids for.
+constexpr int kTreeMinPages = 16, kTreeMaxPages = 1024;
+// Query rows of one workgroup, at most.
+constexpr int kTreeRows = 256;
+
+dbt_status check_tree(const dbt_kv *kv, const dbt_tree *t, int *nodes) {
+  if (!t || !t->h_nodes) return fail(DBT_ERR_ARG, "tree or its node counts are NULL");
+  const dbt_config &cf = kv->m->cfg;
+  if (t->batch <= 0 || t->batch > cf.max_batch) return fail(DBT_ERR_ARG, "batch %d out of [1, %d]", t->batch, cf.max_batch);
+  long long sum = 0;
+  for (int b = 0; b < t->batch; ++b) {
+    if (t->h_nodes[b] < 0 || t->h_nodes[b] > DBT_TREE_NODES)
+      return fail(DBT_ERR_ARG, "sequence %d has %d nodes, outside [0, %d]", b, t->h_nodes[b], DBT_TREE_NODES);
+    sum += t->h_nodes[b];
+  }
+  if (sum == 0) return fail(DBT_ERR_ARG, "the tree has no nodes");
+  *nodes = (int)sum;
+  return DBT_OK;
+}
+
+// Whether every sequence of the tree can grow by its nodes.
+dbt_status check_tree_growth(const dbt_kv *kv, const dbt_tree *t) {
+  long long need = 0;
+  for (int b = 0; b < t->batch; ++b) {
+    const long long len = (long long)kv->len[b] + t->h_nodes[b];
+    if (len > kv->m->cfg.max_pos) return fail(DBT_ERR_SHAPE, "sequence %d would exceed max_pos", b);
+    const int pages = (int)((len + kPage - 1) / kPage);
+    if (pages > kv->mpps) return fail(DBT_ERR_NO_PAGES, "sequence %d page table full", b);
+    need += std::max(0, pages - (int)kv->table[b].size());
+  }
+  if (need > (long long)kv->free_pages.size())
+    return fail(DBT_ERR_NO_PAGES, "need %lld free pages, have %zu", need, kv->free_pages.size());
+  return DBT_OK;
+}
+
+// The pages the nodes of every sequence need (checked by check_tree_growth).
+void take_tree_pages(dbt_kv *kv, const dbt_tree *t) {
+  for (int b = 0; b < t->batch; ++b) {
+    const size_t pages = (size_t)(kv->len[b] + t->h_nodes[b] + kPage - 1) / kPage;
+    while (kv->table[b].size() < pages) {
+      const int p = kv->take_page();
+      kv->table[b].push_back(p);
+      kv->pending.push_back({b, (int)kv->table[b].size() - 1, p});
+    }
+  }
+}
+
+// Sequence b keeps its first `keep` pages.
+void give_back_pages(dbt_kv *kv, int b, size_t keep) {
+  for (size_t i = keep; i < kv->table[b].size(); ++i) kv->free_pages.push(kv->table[b][i]);
+  if (kv->table[b].size() > keep) kv->table[b].resize(keep);
+  // entries of pages given back may still sit in the pending list; they are
+  // harmless (a later take re-sends the slot) but drop those of this sequence
+  kv->pending.erase(std::remove_if(kv->pending.begin(), kv->pending.end(),
+                                   [&](const dbt_kv::Upd &u) { return u.b == b && (size_t)u.slot >= keep; }),
+                    kv->pending.end());
+}
+
+// Rows of partial results (of every KV head) a call of up to `nodes` nodes of
+// up to `pages` pages each can need.  Splits are chosen for at most four
+// rounds of kComputeUnits workgroups of kTreeRows rows beyond one per sequence
+// (plan_tree), or by kTreeMaxPages where that asks for more.
+size_t tree_partial_rows(const dbt_config &c, int nodes, int pages) {
+  const size_t rows = (size_t)nodes * (1 + n_branches(c)) * c.n_q_heads;
+  const size_t rounds = (size_t)8 * kComputeUnits * kTreeRows;
+  return std::min(rows * ((pages + kTreeMinPages - 1) / kTreeMinPages),
+                  std::max(rounds, rows * ((pages + kTreeMaxPages - 1) / kTreeMaxPages)));
+}
+
+struct TreeLayout {
+  size_t map, opart, ostat, total;
+};
+TreeLayout tree_layout(const dbt_config &c, int nodes) {
+  TreeLayout L;
+  const int pages = (c.max_pos + kPage - 1) / kPage;
+  const size_t rows = pages > kTreeMinPages ? tree_partial_rows(c, nodes, pages) : 0;
+  L.map = 0;
+  L.opart = align256((size_t)nodes * sizeof(PromptRow));
+  L.ostat = L.opart + align256(rows * c.head_dim * 4);
+  L.total = L.ostat + align256(rows * 2 * 4);
+  return L;
+}
+
+// base[b]: positions of sequence b before its nodes.
+TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths, const int *base, char *ws) {
+  const dbt_config &cf = m->cfg;
+  TreePlan p;
+  p.parents = t->parents;
+  p.nodes = nodes;
+  const TreeLayout L = tree_layout(cf, nodes);
+  p.map = (PromptRow *)(ws + L.map);
+  p.opart = (float *)(ws + L.opart);
+  p.ostat = (float *)(ws + L.ostat);
+  const int G = cf.n_q_heads / cf.n_kv_heads;
+  auto pages = [&](int b) { return (base[b] + t->h_nodes[b] + kPage - 1) / kPage; };
+  int longest = 1;
+  for (int b = 0; b < t->batch; ++b)
+    if (t->h_nodes[b]) longest = std::max(longest, pages(b));
+  p.pages_per_split = std::min(longest, kTreeMaxPages);
+  p.max_splits = (longest + p.pages_per_split - 1) / p.pages_per_split;
+  int off = 0, part = 0;
+  for (int b = 0; b < t->batch; ++b) {
+    const int n = t->h_nodes[b];
+    if (n == 0) continue;
+    p.max_nodes = std::max(p.max_nodes, n);
+    if (p.groups.empty() || p.groups.back().n == kTreeSeqs) {
+      p.groups.emplace_back();
+      p.groups.back().n = 0;
+      p.groups.back().off[0] = off;
+    }
+    TreeSeqs &g = p.groups.back();
+    g.seq[g.n] = b;
+    g.base[g.n] = base[b];
+    g.part[g.n] = part;
+    off += n;
+    const int ns = (pages(b) + p.pages_per_split - 1) / p.pages_per_split;
+    if (ns > 1) part += ns * n * n_paths * G;
+    g.off[++g.n] = off;
+  }
+  return p;
+}
+
 }  // namespace
 
 // ===========================================================================
@@ -1448,14 +1610,8 @@ dbt_status dbt_kv_truncate(dbt_kv *kv, int32_t b, int32_t len) {
   if (b < 0 || b >= kv->m->cfg.max_batch) return fail(DBT_ERR_ARG, "sequence %d out of range", b);
   if (len < 0 || len > kv->len[b]) return fail(DBT_ERR_ARG, "len %d outside [0, %d]", len, kv->len[b]);
   const size_t keep = (len + kPage - 1) / kPage;
-  for (size_t i = keep; i < kv->table[b].size(); ++i) kv->free_pages.push(kv->table[b][i]);
-  kv->table[b].resize(keep);
+  give_back_pages(kv, b, keep);
   kv->len[b] = len;
-  // entries of pages given back may still sit in the pending list; they are
-  // harmless (a later take re-sends the slot) but drop those of this sequence
-  kv->pending.erase(std::remove_if(kv->pending.begin(), kv->pending.end(),
-                                   [&](const dbt_kv::Upd &u) { return u.b == b && (size_t)u.slot >= keep; }),
-                    kv->pending.end());
   if (kv->m->bnd_kv == kv) kv->m->bnd_kv = nullptr;
   return DBT_OK;
 }
@@ -1662,6 +1818,212 @@ dbt_status dbt_boundary(dbt_model *m, dbt_kv *kv, int32_t batch, dbt_step_out *o
   hipStream_t st = (hipStream_t)stream;
   if ((s = ensure_device(m, st))) return s;
   return boundary_impl(m, kv, batch, out, make_sinks(m, batch, round16(batch), out, false, true), false, st);
+}
+
+// ---- drafted tokens ----
+
+size_t dbt_tree_workspace_bytes(const dbt_config *cfg, int32_t nodes) {
+  if (check_config(cfg) != DBT_OK) return 0;
+  if (nodes <= 0) {
+    fail(DBT_ERR_ARG, "nodes must be positive");
+    return 0;
+  }
+  return tree_layout(*cfg, nodes).total;
+}
+
+dbt_status dbt_tree_reserve(dbt_kv *kv, const dbt_tree *tree) try {
+  if (!kv) return fail(DBT_ERR_ARG, "cache is NULL");
+  int nodes;
+  dbt_status s = check_tree(kv, tree, &nodes);
+  if (s || (s = check_tree_growth(kv, tree))) return s;
+  take_tree_pages(kv, tree);
+  for (int b = 0; b < tree->batch; ++b) kv->len[b] += tree->h_nodes[b];
+  if (kv->m->bnd_kv == kv) kv->m->bnd_kv = nullptr;
+  return DBT_OK;
+} catch (const std::exception &) {
+  return fail(DBT_ERR_ARG, "out of host memory");
+}
+
+dbt_status dbt_tree_attention(dbt_kv *kv, int32_t layer, const dbt_tree *tree, int32_t n_paths, const void *q,
+                              void *out, void *workspace, dbt_stream stream) try {
+  if (!kv || !q || !out) return fail(DBT_ERR_ARG, "NULL argument");
+  const dbt_config &cf = kv->m->cfg;
+  int nodes;
+  dbt_status s = check_tree(kv, tree, &nodes);
+  if (s) return s;
+  if (!tree->parents) return fail(DBT_ERR_ARG, "parents are NULL");
+  if (layer < 0 || layer >= cf.n_layers) return fail(DBT_ERR_ARG, "layer %d out of range", layer);
+  if (n_paths < 1 || n_paths > 1 + n_branches(cf)) return fail(DBT_ERR_ARG, "n_paths %d out of [1, %d]", n_paths, 1 + n_branches(cf));
+  if (((uintptr_t)q | (uintptr_t)out) & 15) return fail(DBT_ERR_ARG, "q or out not 16-byte aligned");
+  if (!workspace || ((uintptr_t)workspace & 255)) return fail(DBT_ERR_ARG, "workspace NULL or not 256-byte aligned");
+  std::vector<int> base(tree->batch);
+  for (int b = 0; b < tree->batch; ++b) {
+    base[b] = kv->len[b] - tree->h_nodes[b];
+    if (base[b] < 0) return fail(DBT_ERR_ARG, "sequence %d has %d positions and %d nodes", b, kv->len[b], tree->h_nodes[b]);
+  }
+  hipStream_t st = (hipStream_t)stream;
+  if ((s = flush(kv, nullptr, 0, st))) return s;
+  TreeAttn a{};
+  a.Q = q;
+  a.q32 = cf.dtype == DBT_F32;
+  a.O = out;
+  a.path_rows = nodes;
+  a.kv = kv_layer(kv, layer);
+  a.n_q = cf.n_q_heads;
+  a.np = n_paths;
+  a.dtype = cf.dtype;
+  HIPCHK(tree_attn(plan_tree(kv->m, tree, nodes, n_paths, base.data(), (char *)workspace), a, st));
+  return DBT_OK;
+} catch (const std::exception &) {
+  return fail(DBT_ERR_ARG, "out of host memory");
+}
+
+dbt_status dbt_decode_tree(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, const dbt_tree *tree, int32_t branch_on,
+                           dbt_step_out *out, void *workspace, dbt_stream stream) try {
+  dbt_status s = check_model_kv(m, kv);
+  if (s) return s;
+  const dbt_config &cf = m->cfg;
+  int nodes;
+  if ((s = check_tree(kv, tree, &nodes))) return s;
+  if (!tree->parents) return fail(DBT_ERR_ARG, "parents are NULL");
+  if (!in) return fail(DBT_ERR_ARG, "step input is NULL");
+  if (in->batch != nodes) return fail(DBT_ERR_ARG, "batch %d, and the tree has %d nodes", in->batch, nodes);
+  if (nodes > cf.max_batch) return fail(DBT_ERR_ARG, "%d nodes exceed max_batch %d", nodes, cf.max_batch);
+  const bool on = branch_on != 0;
+  if (cf.has_embeddings) {
+    if (!in->tokens) return fail(DBT_ERR_ARG, "tokens are NULL");
+  } else {
+    if (!in->h1_in || (on && !in->h2_in)) return fail(DBT_ERR_ARG, "residual inputs are NULL");
+  }
+  if (!workspace || ((uintptr_t)workspace & 255)) return fail(DBT_ERR_ARG, "workspace NULL or not 256-byte aligned");
+  if ((s = check_tree_growth(kv, tree))) return s;
+  hipStream_t st = (hipStream_t)stream;
+  if ((s = ensure_device(m, st))) return s;  // before any state changes
+  m->bnd_kv = nullptr;
+  // a call that fails gives back the pages it took
+  struct Undo {
+    dbt_kv *kv;
+    std::vector<size_t> pages;
+    ~Undo() {
+      for (size_t b = 0; b < pages.size(); ++b)
+        if (kv->table[b].size() > pages[b]) give_back_pages(kv, (int)b, pages[b]);
+    }
+  } undo{kv, {}};
+  for (int b = 0; b < tree->batch; ++b) undo.pages.push_back(kv->table[b].size());
+  take_tree_pages(kv, tree);
+  if ((s = flush(kv, nullptr, 0, st))) return s;
+  const int nb = n_branches(cf), R = nodes, Rp = round16(nodes);
+  const Rows rows{R, Rp, 0, on ? 1 + nb : 1};
+  TreePlan plan = plan_tree(m, tree, nodes, cf.compute_matched ? 1 : rows.np, kv->len.data(), (char *)workspace);
+  for (const TreeSeqs &g : plan.groups) HIPCHK(launch_tree_rows(g, plan.parents, plan.map, st));
+  if ((s = load_inputs(m, kv, in, in->tokens, rows, st))) return s;
+  LayerCall lc{};
+  lc.rows = rows;
+  lc.mode = on ? MODE_GROUPED : MODE_PRIMARY;
+  lc.rows_layout = (1 + nb) * Rp;
+  lc.last_norm = true;
+  lc.out = out;
+  lc.tree = &plan;
+  // (the last layer is the first to write an output, after every read of the
+  // inputs but the tree's parents)
+  const Sinks k = make_sinks(m, R, Rp, out, true, on, Span{tree->parents, (size_t)nodes * sizeof(int)});
+  lc.ho = k.ho;
+  for (int l = 0; l < cf.n_layers; ++l)
+    if ((s = run_layer(m, kv, l, lc, st))) return s;
+  if (cf.vocab > 0 && (s = lm_head(m, rows, k, st))) return s;
+  if (out) {
+    if ((s = readout(m, R, Rp, on, out, k, st))) return s;
+    if (k.copy_h1 && (s = copy_rows(out->h1_out, m->at<float>(m->L.S), R, cf.d_model, st))) return s;
+    if (on && k.copy_h2 && (s = copy_branch_rows(m, out->h2_out, R, Rp, st))) return s;
+  }
+  undo.pages.clear();
+  for (int b = 0; b < tree->batch; ++b) kv->len[b] += tree->h_nodes[b];
+  return DBT_OK;
+} catch (const std::exception &) {
+  return fail(DBT_ERR_ARG, "out of host memory");
+}
+
+dbt_status dbt_tree_accept(int32_t batch, const int32_t *h_nodes, const int32_t *h_parents, const int32_t *h_tokens,
+                           const int32_t *h_drawn, int32_t *h_path, int32_t *h_kept, int32_t *h_next) {
+  if (!h_nodes || !h_parents || !h_tokens || !h_drawn || !h_path || !h_kept) return fail(DBT_ERR_ARG, "NULL argument");
+  if (batch <= 0) return fail(DBT_ERR_ARG, "batch must be positive");
+  for (int b = 0; b < batch; ++b)
+    if (h_nodes[b] < 0 || h_nodes[b] > DBT_TREE_NODES)
+      return fail(DBT_ERR_ARG, "sequence %d has %d nodes, outside [0, %d]", b, h_nodes[b], DBT_TREE_NODES);
+  size_t off = 0, out = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int n = h_nodes[b];
+    const int32_t *up = h_parents + off, *tok = h_tokens + off, *drawn = h_drawn + off;
+    int kept = 0, next = -1;
+    // (children come after their parents: one pass over the nodes)
+    for (int i = 0, at = 0; i < n; ++i) {
+      if (i > 0 && !(up[i] == at && tok[i] == drawn[at])) continue;
+      at = i;
+      h_path[out + kept++] = i;
+      next = drawn[i];
+    }
+    h_kept[b] = kept;
+    if (h_next) h_next[b] = next;
+    off += n;
+    out += kept;
+  }
+  return DBT_OK;
+}
+
+dbt_status dbt_kv_keep(dbt_kv *kv, const dbt_tree *tree, const int32_t *h_kept, const int32_t *h_path,
+                       dbt_stream stream) try {
+  if (!kv || !h_kept || !h_path) return fail(DBT_ERR_ARG, "NULL argument");
+  const dbt_config &cf = kv->m->cfg;
+  int nodes;
+  dbt_status s = check_tree(kv, tree, &nodes);
+  if (s) return s;
+  size_t off = 0;
+  for (int b = 0; b < tree->batch; ++b) {
+    const int n = tree->h_nodes[b];
+    if (n > kv->len[b]) return fail(DBT_ERR_ARG, "sequence %d has %d positions and %d nodes", b, kv->len[b], n);
+    if (h_kept[b] < 0 || h_kept[b] > n) return fail(DBT_ERR_ARG, "sequence %d keeps %d of %d nodes", b, h_kept[b], n);
+    for (int j = 0; j < h_kept[b]; ++j) {
+      const int i = h_path[off + j];
+      if (i < 0 || i >= n || (j > 0 && i <= h_path[off + j - 1]))
+        return fail(DBT_ERR_ARG, "kept nodes of sequence %d are not ascending indices below %d", b, n);
+    }
+    off += h_kept[b];
+  }
+  hipStream_t st = (hipStream_t)stream;
+  if ((s = flush(kv, nullptr, 0, st))) return s;
+  KeepSeqs ks;
+  ks.n = 0;
+  const KVRef first = kv_layer(kv, 0);
+  const size_t layer_elems = (size_t)kv->num_pages * cf.n_kv_heads * kPage * cf.head_dim;
+  off = 0;
+  for (int b = 0; b < tree->batch; ++b) {
+    const int n = tree->h_nodes[b], kept = h_kept[b];
+    int j0 = 0;  // (kept nodes that are in place already)
+    while (j0 < kept && h_path[off + j0] == j0) ++j0;
+    if (j0 < kept) {
+      const int i = ks.n++;
+      ks.seq[i] = b;
+      ks.base[i] = kv->len[b] - n;
+      ks.first[i] = (uint8_t)j0;
+      ks.count[i] = (uint8_t)kept;
+      for (int j = 0; j < kept; ++j) ks.path[i][j] = (uint8_t)h_path[off + j];
+      if (ks.n == kKeepSeqs) {
+        HIPCHK(launch_tree_keep(ks, first, cf.n_layers, layer_elems, cf.dtype, st));
+        ks.n = 0;
+      }
+    }
+    off += kept;
+  }
+  HIPCHK(launch_tree_keep(ks, first, cf.n_layers, layer_elems, cf.dtype, st));
+  for (int b = 0; b < tree->batch; ++b) {
+    const int len = kv->len[b] - tree->h_nodes[b] + h_kept[b];
+    give_back_pages(kv, b, (size_t)(len + kPage - 1) / kPage);
+    kv->len[b] = len;
+  }
+  if (kv->m->bnd_kv == kv) kv->m->bnd_kv = nullptr;
+  return DBT_OK;
+} catch (const std::exception &) {
+  return fail(DBT_ERR_ARG, "out of host memory");
 }
 
 dbt_status dbt_stage_timing(dbt_model *m, int32_t stage, int32_t enable) {

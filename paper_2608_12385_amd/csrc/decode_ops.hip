@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256) void k_prompt_plan(Pack pk, int tp, PromptRow 
       else hi = mid;
     }
     const int seq = pk.seq0 + lo;
-    ((int4 *)rows)[i] = make_int4(i - pk.off[lo], seq, i + 1 == pk.off[lo + 1] ? seq : -1, 0);
+    ((int4 *)rows)[i] = make_int4(i - pk.off[lo], seq, i + 1 == pk.off[lo + 1] ? seq : -1, i - pk.off[lo]);
   }
   int s = 0, j = i;
   for (; s < pk.n; ++s) {
@@ -309,8 +309,9 @@ __global__ void k_qkv_finish(QKVFinish f) {
     return;
   }
   // keys and values (primary only): cache slot of position pos
-  const int page = f.kv.page_table[(size_t)seq * f.kv.mpps + pos / 16];
-  const int slot = pos % 16;
+  const int at = f.pos_arr ? pos : f.prompt[b].slot;
+  const int page = f.kv.page_table[(size_t)seq * f.kv.mpps + at / 16];
+  const int slot = at % 16;
   const int j = pi - nqp;
   T *kp = (T *)f.kv.k;
   T *vp = (T *)f.kv.v;

@@ -33,9 +33,11 @@ enum Mode { MODE_GROUPED = 0, MODE_PRIMARY = 1, MODE_BRANCH = 2 };
 
 // Prompts of several sequences are packed into one pass: row r of the pass is
 // position pos of sequence seq; keep is the sequence at its prompt's last
-// row (whose primary intermediates are kept for the boundary) and -1 elsewhere.
+// row (whose primary intermediates are kept for the boundary) and -1 elsewhere;
+// slot is the cache position of its key and value (pos itself in a prompt; a
+// drafted node's rotary position is its depth, its slot its place in the list).
 struct PromptRow {
-  int pos, seq, keep, unused;
+  int pos, seq, keep, slot;
 };
 // One attention tile of a packed pass: query positions q0 .. of a prompt of T
 // positions of sequence seq, whose position 0 is row row0 of the pass.
@@ -349,6 +351,48 @@ bool prompt_shares_pages(int n_q, int n_kv, int len, int dtype);
 // Query positions per workgroup of the prompt kernels.
 int prompt_tile_positions(int n_q, int n_kv, bool shared);
 hipError_t launch_attn_prefill(const PromptAttn &a, hipStream_t st);
+
+// ---- drafted tokens (tree_attention.hip) ----
+// Sequences of a tree call that have nodes: sequence seq[i] has base[i]
+// positions before its nodes, which are rows off[i] .. off[i + 1] - 1 of the
+// call; its partial results start at row part[i] (per KV head, split and query row).
+constexpr int kTreeSeqs = 128;
+constexpr int kTreeNodes = 64;  // DBT_TREE_NODES: one lane, one bit of a line of ancestors each
+struct TreeSeqs {
+  int n;
+  int seq[kTreeSeqs], base[kTreeSeqs], off[kTreeSeqs + 1], part[kTreeSeqs];
+};
+// Row map of the nodes (position, sequence, slot; kept nowhere).
+hipError_t launch_tree_rows(const TreeSeqs &s, const int *parents, PromptRow *rows, hipStream_t st);
+struct TreeAttn {
+  TreeSeqs s;
+  const int *parents;
+  const void *Q;      // row (path p, node row r): Q + ((size_t)p * path_rows + r) * n_q * d_h
+  bool q32;           // Q is fp32 (else the cache's type)
+  void *O;            // as Q, in the cache's type
+  size_t path_rows;
+  KVRef kv;
+  int n_q, np;        // query heads, paths
+  int dtype;
+  int pages_per_split;  // a sequence of P pages is read in ceil(P / this) equal splits
+  int max_splits;
+  int max_nodes;      // of one sequence
+  float *opart;       // [partial row][n_kv][d_h]
+  float *ostat;       // [partial row][n_kv][2]
+};
+hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st);
+// Kept nodes of up to kKeepSeqs sequences: node path[i][j] of sequence seq[i]
+// moves to position base[i] + j, j = first[i] .. count[i] - 1 (those before
+// stay where they are).
+constexpr int kKeepSeqs = 32;
+struct KeepSeqs {
+  int n;
+  int seq[kKeepSeqs], base[kKeepSeqs];
+  uint8_t first[kKeepSeqs], count[kKeepSeqs], path[kKeepSeqs][kTreeNodes];
+};
+// kv: the first layer's pages; the layers' lie layer_elems elements apart.
+hipError_t launch_tree_keep(const KeepSeqs &s, const KVRef &kv, int n_layers, size_t layer_elems, int dtype,
+                            hipStream_t st);
 
 // ---- cache fill ----
 hipError_t launch_kv_fill(KVRef kv, int seq, int start, int count, const void *ksrc,
