@@ -220,9 +220,13 @@ class _Cache:
             self.tree_workspace = torch.empty(binding.dbt_tree_workspace_bytes(cfg, sum(self.nodes)), dtype=torch.uint8,
                                               device="cuda")
         else:
-            self.paths = binding.make_paths(_kept(c))
+            # the nodes that a pass drops are grown again before the next one
+            kept = _kept(c)
+            self.paths = binding.make_paths(kept)
+            self.tree = binding.make_tree(self.nodes)
+            self.grow = binding.make_tree([n - len(p) for n, p in zip(self.nodes, kept)])
             for b in range(c["batch"]):
-                binding.dbt_kv_truncate(self.kv, b, self.lens[b])
+                binding.dbt_kv_truncate(self.kv, b, self.lens[b] + len(kept[b]))
 
     def __del__(self):
         if getattr(self, "kv", None):
@@ -294,7 +298,7 @@ def run(s):
                                      s.tree_workspace.data_ptr(), stream)
             return s.out
         if op == "keep":
-            s.lib.dbt_tree_reserve(s.kv, s.tree)
+            s.lib.dbt_tree_reserve(s.kv, s.grow)
             s.lib.dbt_kv_keep(s.kv, s.tree, s.paths, stream)
             return {"k": s.k, "v": s.v}
         s.lib.dbt_sample(s.input, s.token.data_ptr(), s.prob.data_ptr(), s.workspace.data_ptr(), stream)
