@@ -286,14 +286,15 @@ dbt_status dbt_decode_step_noalloc(dbt_model *m, dbt_kv *kv, const dbt_step_in *
  * (dbt_kv_truncate), other calls take those positions for ordinary ones. */
 
 /* The drafted nodes of sequences 0..batch-1, sequence after sequence.  A
- * sequence without nodes takes no part.  parents[i] is the index, among its own
+ * sequence without nodes takes no part; dbt_tree_attention and dbt_decode_tree
+ * need one node at least.  parents[i] is the index, among its own
  * sequence's nodes, of the node that node i follows, or -1 when it follows the
  * cached positions; it must be smaller than the node's own index (any other
  * value reads as -1). */
 #define DBT_TREE_NODES 64
 typedef struct {
   int32_t batch;
-  const int32_t *h_nodes; /* HOST [batch]: nodes per sequence, 0..DBT_TREE_NODES; at least one in all */
+  const int32_t *h_nodes; /* HOST [batch]: nodes per sequence, 0..DBT_TREE_NODES */
   const int32_t *parents; /* [sum h_nodes] */
 } dbt_tree;
 

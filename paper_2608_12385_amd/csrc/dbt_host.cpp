@@ -1371,7 +1371,8 @@ constexpr int kTreeMinPages = 16, kTreeMaxPages = 1024;
 // Query rows of one workgroup, at most.
 constexpr int kTreeRows = 256;
 
-dbt_status check_tree(const dbt_kv *kv, const dbt_tree *t, int *nodes) {
+// may_be_empty: calls without a launch over the nodes
+dbt_status check_tree(const dbt_kv *kv, const dbt_tree *t, int *nodes, bool may_be_empty = false) {
   if (!t || !t->h_nodes) return fail(DBT_ERR_ARG, "tree or its node counts are NULL");
   const dbt_config &cf = kv->m->cfg;
   if (t->batch <= 0 || t->batch > cf.max_batch) return fail(DBT_ERR_ARG, "batch %d out of [1, %d]", t->batch, cf.max_batch);
@@ -1381,7 +1382,7 @@ dbt_status check_tree(const dbt_kv *kv, const dbt_tree *t, int *nodes) {
       return fail(DBT_ERR_ARG, "sequence %d has %d nodes, outside [0, %d]", b, t->h_nodes[b], DBT_TREE_NODES);
     sum += t->h_nodes[b];
   }
-  if (sum == 0) return fail(DBT_ERR_ARG, "the tree has no nodes");
+  if (sum == 0 && !may_be_empty) return fail(DBT_ERR_ARG, "the tree has no nodes");
   *nodes = (int)sum;
   return DBT_OK;
 }
@@ -1834,7 +1835,7 @@ size_t dbt_tree_workspace_bytes(const dbt_config *cfg, int32_t nodes) {
 dbt_status dbt_tree_reserve(dbt_kv *kv, const dbt_tree *tree) try {
   if (!kv) return fail(DBT_ERR_ARG, "cache is NULL");
   int nodes;
-  dbt_status s = check_tree(kv, tree, &nodes);
+  dbt_status s = check_tree(kv, tree, &nodes, true);
   if (s || (s = check_tree_growth(kv, tree))) return s;
   take_tree_pages(kv, tree);
   for (int b = 0; b < tree->batch; ++b) kv->len[b] += tree->h_nodes[b];
@@ -1975,7 +1976,7 @@ dbt_status dbt_kv_keep(dbt_kv *kv, const dbt_tree *tree, const int32_t *h_kept, 
   if (!kv || !h_kept || !h_path) return fail(DBT_ERR_ARG, "NULL argument");
   const dbt_config &cf = kv->m->cfg;
   int nodes;
-  dbt_status s = check_tree(kv, tree, &nodes);
+  dbt_status s = check_tree(kv, tree, &nodes, true);
   if (s) return s;
   size_t off = 0;
   for (int b = 0; b < tree->batch; ++b) {
