@@ -1,5 +1,5 @@
 // Attention over an fp32 paged cache on the fp32 matrix instruction
-// (v_mfma_f32_16x16x4_f32), shared by the decode and the prompt kernel:
+// (v_mfma_f32_16x16x4_f32), shared by the decode, prompt and tree kernels:
 // sixteen query rows against a range of pages, the pages dealt to the
 // workgroup's waves, one online softmax per wave, merged through LDS.
 //
@@ -43,14 +43,30 @@ struct F32Merge {
   }
 };
 
+// Which positions a lane's row sees; row(q): what row q of the sixteen sees.
+struct SeesBefore {  // 0 .. seen - 1
+  int seen;
+  __device__ __forceinline__ bool operator()(int pos) const { return pos < seen; }
+  __device__ __forceinline__ SeesBefore row(int q) const { return {__shfl(seen, q, 64)}; }
+};
+struct SeesLine {  // 0 .. base - 1, and base + j where bit j of the line is set
+  int base;
+  uint64_t line;
+  __device__ __forceinline__ bool operator()(int pos) const {
+    return pos < base || (pos - base < 64 && ((line >> (pos - base)) & 1));
+  }
+  __device__ __forceinline__ SeesLine row(int q) const { return {base, __shfl(line, q, 64)}; }
+};
+
 // qp: this lane's query row (row r = lane & 15; live = false: a stand-in whose
-// results are not used); it sees keys 0 .. seen - 1.  Pages [pb, pe) of ptab;
-// positions >= valid hold no key (stale slots).  CAUSAL: rows see different
-// numbers of keys, but all of those before the last page.  Ends with a barrier.
-template <int NC, bool CAUSAL>
-__device__ __forceinline__ void attn_f32(F32Merge<NC> &mg, const float *qp, bool live, int seen, int valid,
-                                         const float *kbase, const float *vbase, const int *ptab, int pb, int pe,
-                                         int n_kv, int g, int DH) {
+// results are not used).  Pages [pb, pe) of ptab; positions >= valid hold no
+// key (stale slots).  Every row sees the valid keys of the pages before
+// `apart`; from there (at most kWavesF32Attn pages: each a wave's last one) rows see
+// different keys.  Ends with a barrier.
+template <int NC, typename SEES>
+__device__ __forceinline__ void attn_f32(F32Merge<NC> &mg, const float *qp, bool live, const SEES &sees, int apart,
+                                         int valid, const float *kbase, const float *vbase, const int *ptab, int pb,
+                                         int pe, int n_kv, int g, int DH) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int r = lane & 15, gq = lane >> 4;
   const float scale = kLog2e / sqrtf((float)DH);
@@ -82,7 +98,7 @@ __device__ __forceinline__ void attn_f32(F32Merge<NC> &mg, const float *qp, bool
   int next = j + kWavesF32Attn < pe ? ptab[j + kWavesF32Attn] : 0;  // page ids run one turn further ahead
   if (j < pe) load(ptab[j]);
   float p[4] = {0.f, 0.f, 0.f, 0.f};
-  bool apart = false;  // the last page holds values that are not finite (CAUSAL)
+  int odd_page = -1;  // this wave's page from `apart` on that holds values which are not finite
   for (; j < pe; j += kWavesF32Attn) {
     floatx4 s = {0.f, 0.f, 0.f, 0.f};
     if (16 * NC > DH && 16 * (NC - 1) + 4 * gq >= DH) k[NC - 1] = floatx4{0.f, 0.f, 0.f, 0.f};  // (infinity * 0)
@@ -100,7 +116,7 @@ __device__ __forceinline__ void attn_f32(F32Merge<NC> &mg, const float *qp, bool
     float mt = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      s[i] = p0 + i < seen ? s[i] * scale : -INFINITY;
+      s[i] = sees(p0 + i) ? s[i] * scale : -INFINITY;
       mt = fmaxf(mt, s[i]);
     }
     const float m_new = fmaxf(m_run, rows4_max(mt));
@@ -119,10 +135,9 @@ __device__ __forceinline__ void attn_f32(F32Merge<NC> &mg, const float *qp, bool
         for (int i = 0; i < 4; ++i)
           if (p0 + i >= valid) vc[c][i] = 0.f;
     }
-    if (CAUSAL && j == pe - 1) {
-      // the page of the tile's own positions: a probability of zero would not
-      // hide a value that is not finite from the rows before it, so such
-      // values are taken out here and added below
+    if (j >= apart) {
+      // a probability of zero would not hide a value that is not finite from
+      // the rows that do not see it, so such values are taken out here and added below
       bool odd = false;
 #pragma unroll
       for (int c = 0; c < NC; ++c)
@@ -132,7 +147,7 @@ __device__ __forceinline__ void attn_f32(F32Merge<NC> &mg, const float *qp, bool
             vc[c][i] = 0.f;
             odd = true;
           }
-      apart = __any(odd);
+      if (__any(odd)) odd_page = j;
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -141,19 +156,20 @@ __device__ __forceinline__ void attn_f32(F32Merge<NC> &mg, const float *qp, bool
       for (int i = 0; i < 4; ++i) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vc[c][i], p[i], acc[c], 0, 0, 0);
     }
   }
-  if (CAUSAL && apart) {  // row by row, the keys it sees
-    const int p0 = 16 * (pe - 1) + 4 * gq;
-    const float *vp = vbase + ((size_t)ptab[pe - 1] * n_kv + g) * 16 * DH;
+  if (odd_page >= 0) {  // row by row, the keys it sees
+    const int p0 = 16 * odd_page + 4 * gq;
+    const float *vp = vbase + ((size_t)ptab[odd_page] * n_kv + g) * 16 * DH;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const floatx4 w = *(const floatx4 *)(vp + voff[c]);
 #pragma unroll 1
       for (int row = 0; row < 16; ++row) {
-        const int see = min(__shfl(seen, row, 64), valid);
+        const SEES its = sees.row(row);
         floatx4 o = acc[c];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          o = __builtin_amdgcn_mfma_f32_16x16x4f32(p0 + i < see && !(fabsf(w[i]) < INFINITY) ? w[i] : 0.f, p[i], o, 0, 0, 0);
+          o = __builtin_amdgcn_mfma_f32_16x16x4f32(
+              its(p0 + i) && p0 + i < valid && !(fabsf(w[i]) < INFINITY) ? w[i] : 0.f, p[i], o, 0, 0, 0);
         if (r == row) acc[c] = o;
       }
     }

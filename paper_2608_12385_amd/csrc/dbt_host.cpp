@@ -1365,11 +1365,13 @@ dbt_status decode_step_impl(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, int
 
 // ---- drafted tokens ----
 
-// Pages a tree's attention reads per workgroup: at least kTreeMinPages, the
-// most the kernel holds page ids for.
-constexpr int kTreeMinPages = 16, kTreeMaxPages = 1024;
-// Query rows of one workgroup, at most.
-constexpr int kTreeRows = 256;
+// How a tree's attention splits the cache (plan_tree).  A workgroup fills a
+// compute unit (its stages take most of the LDS), so a call runs in rounds of
+// kComputeUnits workgroups.  In pages of reading time: a workgroup's start, and
+// the merge of the splits (a launch, and each row's partial result written and read).
+constexpr int kTreeMinPages = 2 * kTreeStagePages, kTreeMostPages = kTreeMaxPages - kTreeStagePages;
+constexpr int kTreeRounds = 4, kTreeStart = 6, kTreeMerge = 14, kTreeMergeRows = 8;
+constexpr int kTreeRows = 256;  // query rows of one workgroup, at most
 
 // may_be_empty: calls without a launch over the nodes
 dbt_status check_tree(const dbt_kv *kv, const dbt_tree *t, int *nodes, bool may_be_empty = false) {
@@ -1425,15 +1427,14 @@ void give_back_pages(dbt_kv *kv, int b, size_t keep) {
                     kv->pending.end());
 }
 
-// Rows of partial results (of every KV head) a call of up to `nodes` nodes of
-// up to `pages` pages each can need.  Splits are chosen for at most four
-// rounds of kComputeUnits workgroups of kTreeRows rows beyond one per sequence
-// (plan_tree), or by kTreeMaxPages where that asks for more.
+// Rows of partial results (of every KV head) that a call over up to `nodes`
+// nodes and `pages` pages a sequence can need: splits are chosen for at most
+// kTreeRounds rounds, or are as long as they may be.
 size_t tree_partial_rows(const dbt_config &c, int nodes, int pages) {
   const size_t rows = (size_t)nodes * (1 + n_branches(c)) * c.n_q_heads;
-  const size_t rounds = (size_t)8 * kComputeUnits * kTreeRows;
+  const size_t rounds = (size_t)kTreeRounds * kComputeUnits * kTreeRows;
   return std::min(rows * ((pages + kTreeMinPages - 1) / kTreeMinPages),
-                  std::max(rounds, rows * ((pages + kTreeMaxPages - 1) / kTreeMaxPages)));
+                  std::max(rounds, rows * ((pages + kTreeMostPages - 1) / kTreeMostPages)));
 }
 
 struct TreeLayout {
@@ -1450,10 +1451,63 @@ TreeLayout tree_layout(const dbt_config &c, int nodes) {
   return L;
 }
 
+// Pages per split of a tree call.  Equal splits in as few rounds as they fit,
+// by the estimate above; sequences as long as each other and enough of them
+// are not split.  32 sequences of 4096 positions and 8 KV heads, 64 rows each: one
+// workgroup for each of the 256 (sequence, KV head).
+int tree_pages_per_split(const dbt_config &c, const dbt_tree *t, int n_paths, const int *base) {
+  const int G = c.n_q_heads / c.n_kv_heads;
+  struct Seq { int pages, units; };
+  std::vector<Seq> seqs;
+  int longest = 1, most = 0;
+  long long total = 0, units = 0;
+  for (int b = 0; b < t->batch; ++b) most = std::max(most, t->h_nodes[b]);
+  const int rows = most * n_paths * G, cap = tree_block_rows(rows, c.dtype);
+  for (int b = 0; b < t->batch; ++b) {
+    const int n = t->h_nodes[b];
+    if (n == 0) continue;
+    const Seq s{(base[b] + n + kPage - 1) / kPage, c.n_kv_heads * ((n * n_paths * G + cap - 1) / cap)};
+    seqs.push_back(s);
+    longest = std::max(longest, s.pages);
+    total += (long long)s.pages * s.units;
+    units += s.units;
+  }
+  auto workgroups = [&](int target) {
+    long long w = 0;
+    int each;
+    for (const Seq &s : seqs) w += (long long)s.units * tree_splits(s.pages, target, &each);
+    return w;
+  };
+  // unsplit: the longest sequence, or the rounds of the average one
+  const int whole = std::min(longest, kTreeMostPages);
+  const long long avg = units ? total / units : 0;
+  long long best = std::max<long long>(longest + kTreeStart,
+                                       (workgroups(whole) + kComputeUnits - 1) / kComputeUnits * (avg + kTreeStart));
+  int choice = whole;
+  for (int k = 1; k <= kTreeRounds; ++k) {
+    int lo = kTreeMinPages / kTreeStagePages, hi = (whole + kTreeStagePages - 1) / kTreeStagePages;
+    if (hi * kTreeStagePages > kTreeMostPages) hi = kTreeMostPages / kTreeStagePages;
+    if (lo >= hi || workgroups(hi * kTreeStagePages) > (long long)k * kComputeUnits) continue;
+    while (lo < hi) {  // the shortest splits that fit k rounds
+      const int mid = (lo + hi) / 2;
+      if (workgroups(mid * kTreeStagePages) <= (long long)k * kComputeUnits) hi = mid;
+      else lo = mid + 1;
+    }
+    const int target = lo * kTreeStagePages;
+    if (target >= whole) continue;
+    const long long cost = (long long)k * (target + kTreeStart) + kTreeMerge + std::min(rows, cap) / kTreeMergeRows;
+    if (cost < best) {
+      best = cost;
+      choice = target;
+    }
+  }
+  return choice;
+}
+
 // base[b]: positions of sequence b before its nodes.
-TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths, const int *base, char *ws) {
+dbt_status plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths, const int *base, char *ws, TreePlan *out) {
   const dbt_config &cf = m->cfg;
-  TreePlan p;
+  TreePlan &p = *out;
   p.parents = t->parents;
   p.nodes = nodes;
   const TreeLayout L = tree_layout(cf, nodes);
@@ -1461,13 +1515,9 @@ TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths
   p.opart = (float *)(ws + L.opart);
   p.ostat = (float *)(ws + L.ostat);
   const int G = cf.n_q_heads / cf.n_kv_heads;
-  auto pages = [&](int b) { return (base[b] + t->h_nodes[b] + kPage - 1) / kPage; };
-  int longest = 1;
-  for (int b = 0; b < t->batch; ++b)
-    if (t->h_nodes[b]) longest = std::max(longest, pages(b));
-  p.pages_per_split = std::min(longest, kTreeMaxPages);
-  p.max_splits = (longest + p.pages_per_split - 1) / p.pages_per_split;
-  int off = 0, part = 0;
+  p.pages_per_split = tree_pages_per_split(cf, t, n_paths, base);
+  int off = 0;
+  long long part = 0;
   for (int b = 0; b < t->batch; ++b) {
     const int n = t->h_nodes[b];
     if (n == 0) continue;
@@ -1480,13 +1530,16 @@ TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths
     TreeSeqs &g = p.groups.back();
     g.seq[g.n] = b;
     g.base[g.n] = base[b];
-    g.part[g.n] = part;
+    g.part[g.n] = (int)part;
     off += n;
-    const int ns = (pages(b) + p.pages_per_split - 1) / p.pages_per_split;
-    if (ns > 1) part += ns * n * n_paths * G;
+    int each;
+    const int ns = tree_splits((base[b] + n + kPage - 1) / kPage, p.pages_per_split, &each);
+    p.max_splits = std::max(p.max_splits, ns);
+    if (ns > 1) part += (long long)ns * n * n_paths * G;
     g.off[++g.n] = off;
   }
-  return p;
+  if (part > 0 && (size_t)part * cf.n_kv_heads * 2 * 4 > L.total - L.ostat) return fail(DBT_ERR_STATE, "internal: tree partials");
+  return DBT_OK;
 }
 
 }  // namespace
@@ -1862,6 +1915,8 @@ dbt_status dbt_tree_attention(dbt_kv *kv, int32_t layer, const dbt_tree *tree, i
     base[b] = kv->len[b] - tree->h_nodes[b];
     if (base[b] < 0) return fail(DBT_ERR_ARG, "sequence %d has %d positions and %d nodes", b, kv->len[b], tree->h_nodes[b]);
   }
+  TreePlan plan;
+  if ((s = plan_tree(kv->m, tree, nodes, n_paths, base.data(), (char *)workspace, &plan))) return s;
   hipStream_t st = (hipStream_t)stream;
   if ((s = flush(kv, nullptr, 0, st))) return s;
   TreeAttn a{};
@@ -1873,7 +1928,7 @@ dbt_status dbt_tree_attention(dbt_kv *kv, int32_t layer, const dbt_tree *tree, i
   a.n_q = cf.n_q_heads;
   a.np = n_paths;
   a.dtype = cf.dtype;
-  HIPCHK(tree_attn(plan_tree(kv->m, tree, nodes, n_paths, base.data(), (char *)workspace), a, st));
+  HIPCHK(tree_attn(plan, a, st));
   return DBT_OK;
 } catch (const std::exception &) {
   return fail(DBT_ERR_ARG, "out of host memory");
@@ -1898,6 +1953,10 @@ dbt_status dbt_decode_tree(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, cons
   }
   if (!workspace || ((uintptr_t)workspace & 255)) return fail(DBT_ERR_ARG, "workspace NULL or not 256-byte aligned");
   if ((s = check_tree_growth(kv, tree))) return s;
+  const int nb = n_branches(cf), R = nodes, Rp = round16(nodes);
+  const Rows rows{R, Rp, 0, on ? 1 + nb : 1};
+  TreePlan plan;
+  if ((s = plan_tree(m, tree, nodes, cf.compute_matched ? 1 : rows.np, kv->len.data(), (char *)workspace, &plan))) return s;
   hipStream_t st = (hipStream_t)stream;
   if ((s = ensure_device(m, st))) return s;  // before any state changes
   m->bnd_kv = nullptr;
@@ -1913,9 +1972,6 @@ dbt_status dbt_decode_tree(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, cons
   for (int b = 0; b < tree->batch; ++b) undo.pages.push_back(kv->table[b].size());
   take_tree_pages(kv, tree);
   if ((s = flush(kv, nullptr, 0, st))) return s;
-  const int nb = n_branches(cf), R = nodes, Rp = round16(nodes);
-  const Rows rows{R, Rp, 0, on ? 1 + nb : 1};
-  TreePlan plan = plan_tree(m, tree, nodes, cf.compute_matched ? 1 : rows.np, kv->len.data(), (char *)workspace);
   for (const TreeSeqs &g : plan.groups) HIPCHK(launch_tree_rows(g, plan.parents, plan.map, st));
   if ((s = load_inputs(m, kv, in, in->tokens, rows, st))) return s;
   LayerCall lc{};

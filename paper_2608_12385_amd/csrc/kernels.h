@@ -374,13 +374,27 @@ struct TreeAttn {
   KVRef kv;
   int n_q, np;        // query heads, paths
   int dtype;
-  int pages_per_split;  // a sequence of P pages is read in ceil(P / this) equal splits
+  int pages_per_split;  // see tree_splits
   int max_splits;
   int max_nodes;      // of one sequence
   float *opart;       // [partial row][n_kv][d_h]
   float *ostat;       // [partial row][n_kv][2]
 };
 hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st);
+// Splits a sequence of `pages` pages is read in and the pages of each (the last
+// may be shorter): about equal, and whole stages of the kernel.
+constexpr int kTreeStagePages = 8;
+constexpr int kTreeMaxPages = 1024;  // pages of one split (their ids are kept in LDS)
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline int tree_splits(int pages, int pages_per_split, int *each) {
+  const int n = (pages + pages_per_split - 1) / pages_per_split;
+  *each = n <= 1 ? pages : ((pages + n - 1) / n + kTreeStagePages - 1) / kTreeStagePages * kTreeStagePages;
+  return n <= 1 ? 1 : (pages + *each - 1) / *each;
+}
+// Query rows (nodes x paths x query heads of a KV head) of one workgroup.
+int tree_block_rows(int rows, int dtype);
 // Kept nodes of up to kKeepSeqs sequences: node path[i][j] of sequence seq[i]
 // moves to position base[i] + j, j = first[i] .. count[i] - 1 (those before
 // stay where they are).

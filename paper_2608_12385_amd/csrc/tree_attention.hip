@@ -6,6 +6,7 @@
 // bits, one per node; a wave finds all of them with one lane per node by
 // pointer doubling: line |= line of the node pointed at, pointer = its pointer,
 // six times for lines of up to 64 nodes.
+#include "attn_f32.h"
 #include "common.h"
 #include "kernels.h"
 
@@ -35,45 +36,408 @@ __global__ __launch_bounds__(64) void k_tree_rows(TreeSeqs s, const int *parents
     ((int4 *)rows)[first + lane] = make_int4(s.base[i] + __popcll(line) - 1, s.seq[i], -1, s.base[i] + lane);
 }
 
-// One workgroup per (query row, query head): scores of 256 keys at a time, one
-// per thread, online softmax over the groups, values summed by dimension.
-template <typename T, typename QT>
-__global__ __launch_bounds__(256) void k_tree_attn_simple(TreeAttn a) {
-  const int i = blockIdx.z, head = blockIdx.y, t = threadIdx.x;
-  const int first = a.s.off[i], n = a.s.off[i + 1] - first;
-  const int node = blockIdx.x / a.np, path = blockIdx.x % a.np;
-  if (node >= n) return;
-  const int DH = a.kv.d_h, base = a.s.base[i], len = base + n, g = head / (a.n_q / a.kv.n_kv);
-  __shared__ float q_s[128], p_s[256], red[16];
-  __shared__ uint64_t line_s;
-  const uint64_t line = t < 64 ? node_line(a.parents + first, n) : 0;
-  if (t == node) line_s = line;
-  const size_t row = ((size_t)path * a.path_rows + first + node) * a.n_q + head;
-  if (t < DH) q_s[t] = ld<QT>((const QT *)a.Q, row * DH + t) * (kLog2e / sqrtf((float)DH));
-  __syncthreads();
-  const int *ptab = a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps;
-  auto sees = [&](int pos) { return pos < base || (pos < len && ((line_s >> (pos - base)) & 1)); };
-  float m = kNoScore, l = 0.f, o = 0.f;
-  for (int p0 = 0; p0 < len; p0 += 256) {
-    const int pos = p0 + t;
-    float s = -INFINITY;
-    if (pos < len && sees(pos)) {
-      const T *k = (const T *)a.kv.k + (((size_t)ptab[pos >> 4] * a.kv.n_kv + g) * 16 + (pos & 15)) * DH;
-      s = 0.f;
-      for (int d = 0; d < DH; ++d) s = fmaf(q_s[d], ld<T>(k, d), s);
-    }
-    const float mn = fmaxf(m, block_max(s, red)), f = exp2f(m - mn), p = exp2f(s - mn);
-    p_s[t] = p;
-    l = l * f + block_sum(p, red);
-    o *= f;
-    m = mn;
-    if (t < DH)
-      for (int j = 0; j < min(256, len - p0); ++j)
-        if (sees(p0 + j))
-          o += p_s[j] * ld<T>((const T *)a.kv.v, (((size_t)ptab[(p0 + j) >> 4] * a.kv.n_kv + g) * DH + t) * 16 + ((p0 + j) & 15));
-    __syncthreads();
+// The place of query row `rho` of a sequence's nodes (node-major, then path,
+// then head of the KV head) in Q and O.
+struct RowPlace {
+  int G, np, first, g, n_q;
+  size_t path_rows;
+  __device__ __forceinline__ size_t operator()(int rho) const {
+    const int t = rho / G;
+    return ((size_t)(t % np) * path_rows + first + t / np) * n_q + g * G + rho % G;
   }
-  if (t < DH) st<T>((T *)a.O, row * DH + t, o / l);
+};
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// Growth of a row's score maximum (base 2) that moves its softmax base.
+constexpr float kLazyMargin = 8.f;
+
+// bf16 cache, d_h = 128.  A workgroup owns RW * RT * 16 query rows of one
+// (sequence, KV head) and a split of its pages.  Eight pages a stage go straight
+// into LDS (64 KB), one stage ahead of the multiplies, so every key and value
+// is fetched once for all rows of the workgroup; wave (rw, kw) multiplies row
+// tiles rw * RT .. + RT - 1 with its share kw of the stage's page pairs, and the KW
+// shares are merged at the end.  Few rows: four waves share the keys (KW = 4,
+// one row tile each holds them all); many: eight waves share the rows.  The
+// arithmetic of a pair is that of the decode kernel: scores S = K Q^T with
+// permuted rows, so that lane (row r, group gq) ends up with eight
+// consecutive positions of one page, which is the operand of O^T = V^T P^T.
+// Rows see different keys only in pages from position `base` on; those pairs
+// take a masked path.
+//
+// Bound: 16 rows and up to 128 per key read at the memory's rate; 256 rows by
+// the vector unit's softmax beside the matrix unit.
+template <int RT, int RW, int KW, typename QT>
+__global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(RW *KW / 4, RW *KW / 4))) void
+k_tree_attn_bf16(TreeAttn a) {
+  constexpr int DH = 128, NW = RW * KW, PP = 4 / KW, PB = 16 * DH;  // PP: pairs of a stage per wave; PB: elements of a page
+  static_assert(kTreeStagePages == 8 && KW * PP == 4, "four pairs per stage");
+  // two sets of stage buffers, separate arrays so that the loads filling one
+  // set are told apart from the reads of the other
+  __shared__ __attribute__((aligned(16))) uint16_t kl0[8 * PB], vl0[8 * PB], kl1[8 * PB], vl1[8 * PB];
+  __shared__ int pid_s[kTreeMaxPages];
+  __shared__ uint64_t line_s[kTreeNodes];
+  __shared__ float ms[KW][RW * RT][16], ls[KW][RW * RT][16];
+  const int i = blockIdx.z, g = blockIdx.y;
+  const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
+  const int G = a.n_q / a.kv.n_kv, rows = n * a.np * G;
+  const int blk = blockIdx.x / a.max_splits, split = blockIdx.x % a.max_splits;
+  const int row0 = blk * (RW * RT * 16);
+  const int npages = (len + 15) >> 4;
+  int each;
+  const int nsplit = tree_splits(npages, a.pages_per_split, &each);
+  if (row0 >= rows || split >= nsplit) return;
+  const int pb = split * each, npg = min(npages, pb + each) - pb;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int rw = wave % RW, kw = wave / RW;
+  const int r = lane & 15, gq = lane >> 4;
+  const int n_kv = a.kv.n_kv;
+  const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
+  const float scale = kLog2e / sqrtf((float)DH);
+  const int *ptab = a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps + pb;
+  for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[k];
+  if (wave == 0) line_s[lane] = node_line(a.parents + first, n);
+  __syncthreads();
+
+  const int wrow = row0 + rw * RT * 16;  // the wave's first row
+  u32x4 qf[RT][4];
+  uint64_t line[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int rho = wrow + rt * 16 + r;
+    const bool live = rho < rows;
+    line[rt] = live ? line_s[rho / (G * a.np)] : 0;
+    const QT *qp = (const QT *)a.Q + place(live ? rho : 0) * DH + gq * 8;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if constexpr (sizeof(QT) == 2) {
+        qf[rt][s] = *(const u32x4 *)(qp + s * 32);
+      } else {  // the projections' queries, rounded once to the cache's type as in a step
+        const float4 x = *(const float4 *)(qp + s * 32), y = *(const float4 *)(qp + s * 32 + 4);
+        qf[rt][s] = u32x4{pack2(x.x, x.y), pack2(x.z, x.w), pack2(y.x, y.y), pack2(y.z, y.w)};
+      }
+      if (!live) qf[rt][s] = u32x4{0, 0, 0, 0};
+    }
+  }
+
+  // K row j of a page holds its 16-byte chunk c at c ^ kswz(j): the score operand
+  // reads rows {0..3, 8..11} (or {4..7, 12..15}) of both pages at one chunk
+  // without bank conflicts.  V rows (one dimension, 32 bytes) need no swizzle.
+  auto kswz = [](int row) { return ((row & 3) | ((row >> 3) << 2)) << 1; };
+  const uint16_t *kbase = (const uint16_t *)a.kv.k, *vbase = (const uint16_t *)a.kv.v;
+  // A stage is 64 loads of 1 KB, four of K and four of V a page: each wave takes
+  // 64 / NW.  Pages past the split's last re-read it (never used unmasked).
+  auto dma = [&](int st, uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < 8 / NW; ++p) {
+      const int page = wave * (8 / NW) + p;
+      const int phys = __builtin_amdgcn_readfirstlane(pid_s[min(st * 8 + page, npg - 1)]);
+      const size_t at = ((size_t)phys * n_kv + g) * PB;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int row = 4 * j + (lane >> 4);
+        __builtin_amdgcn_global_load_lds((const void *)(kbase + at + row * DH + ((lane & 15) ^ kswz(row)) * 8),
+                                         (lds_void *)(kb + page * PB + 4 * j * DH), 16, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        __builtin_amdgcn_global_load_lds((const void *)(vbase + at + 32 * j * 16 + lane * 8),
+                                         (lds_void *)(vb + page * PB + 32 * j * 16), 16, 0, 0);
+    }
+  };
+
+  float m_run[RT];
+  floatx4 acc[RT][8], acc_l[RT];  // acc_l: the sums of the rounded probabilities, by one more value multiply with V = 1
+  const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m_run[rt] = kNoScore;
+    acc_l[rt] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[rt][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  const int kpage = r >> 3, kpos = 8 * ((r >> 2) & 1) + (r & 3);
+  const int vpage = gq >> 1, vpos = 8 * (gq & 1);
+  const bool active = wrow < rows;
+
+  auto pair = [&](int pg0, const uint16_t *kb, const uint16_t *vb, auto masked) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked)::value;
+    u32x4 ka[4], kc[4], vf[8];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      ka[s] = *(const u32x4 *)&kb[(kpage * 16 + kpos) * DH + ((s * 4 + gq) ^ kswz(kpos)) * 8];
+      kc[s] = *(const u32x4 *)&kb[(kpage * 16 + kpos + 4) * DH + ((s * 4 + gq) ^ kswz(kpos + 4)) * 8];
+    }
+    floatx4 sc[RT][2];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      sc[rt][0] = sc[rt][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        sc[rt][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka[s]),
+                                                            __builtin_bit_cast(bf16x8, qf[rt][s]), sc[rt][0], 0, 0, 0);
+        sc[rt][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kc[s]),
+                                                            __builtin_bit_cast(bf16x8, qf[rt][s]), sc[rt][1], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) vf[c] = *(const u32x4 *)&vb[(vpage * DH + c * 16 + r) * 16 + vpos];
+    const int kp0 = (pb + pg0 + vpage) * 16 + vpos;  // position of this lane's first score
+    const bool page_ok = pg0 + vpage < npg;
+    bool odd = false;
+    if (MASKED) {
+      // slots past the sequence may hold anything; values of nodes that are
+      // not finite would reach the rows that do not see them as 0 * infinity,
+      // so they are taken out here and added below
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        vf[c] = mask8(vf[c], kp0, page_ok ? len : kp0);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t x = vf[c][w];
+          const bool lo = (x & 0x7f80u) == 0x7f80u, hi = (x & 0x7f800000u) == 0x7f800000u;
+          if (lo) x &= 0xffff0000u;
+          if (hi) x &= 0x0000ffffu;
+          odd |= lo | hi;
+          vf[c][w] = x;
+        }
+      }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float s[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[e] = sc[rt][0][e];
+        s[4 + e] = sc[rt][1][e];
+      }
+      uint32_t seen = 0xff;
+      if (MASKED) {  // the row's eight positions: before `base`, or on its line
+        const int rel = kp0 - base;
+        seen = !page_ok || rel >= 64 ? 0u
+               : rel >= 0            ? (uint32_t)(line[rt] >> rel) & 0xff
+               : rel > -8            ? (uint32_t)((line[rt] << -rel) | ((1u << -rel) - 1)) & 0xff
+                                     : 0xffu;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!((seen >> e) & 1)) s[e] = -INFINITY;
+      }
+      float mt = s[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) mt = fmaxf(mt, s[e]);
+      // lazy rescaling: a row's base moves only when the pair's maximum exceeds it
+      // by more than kLazyMargin, so exponentials stay <= 2^kLazyMargin
+      const float mt_s = rows4_max(mt) * scale;
+      const bool grow = mt_s > m_run[rt] + kLazyMargin;
+      const float m_new = grow ? mt_s : m_run[rt];
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[e], scale, -m_new));
+      if (__any(grow)) {
+        const float corr = __builtin_amdgcn_exp2f(m_run[rt] - m_new);
+        acc_l[rt] = acc_l[rt] * corr;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[rt][c] = acc[rt][c] * corr;
+      }
+      m_run[rt] = m_new;
+      // (probabilities are rounded to bf16 for the matrix unit; their sum is of the rounded ones)
+      const u32x4 pf = u32x4{pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7])};
+      acc_l[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones),
+                                                          __builtin_bit_cast(bf16x8, pf), acc_l[rt], 0, 0, 0);
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        acc[rt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[c]),
+                                                             __builtin_bit_cast(bf16x8, pf), acc[rt][c], 0, 0, 0);
+      if (MASKED && __any(odd)) {
+        // key by key: lane r + 16 h holds row r's probabilities of group h's positions
+#pragma unroll 1
+        for (int h = 0; h < 4; ++h)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float pk = __shfl(p[e], r + 16 * h, 64);
+            const bool sees = (__shfl(seen, r + 16 * h, 64) >> e) & 1;
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+#pragma unroll
+              for (int d = 0; d < 4; ++d) {
+                const uint16_t x = vb[((h >> 1) * DH + 16 * c + 4 * gq + d) * 16 + 8 * (h & 1) + e];
+                if (sees && (x & 0x7f80) == 0x7f80) acc[rt][c][d] += pk * bf2f(x);
+              }
+          }
+      }
+    }
+  };
+  auto stage = [&](int st, const uint16_t *kb, const uint16_t *vb) __attribute__((always_inline)) {
+    if (!active) return;
+#pragma unroll
+    for (int j = 0; j < PP; ++j) {
+      const int pi = kw * PP + j, pg0 = st * 8 + 2 * pi;
+      if (pg0 >= npg) break;
+      if ((pb + pg0 + 2) * 16 <= base && pg0 + 2 <= npg)
+        pair(pg0, kb + 2 * pi * PB, vb + 2 * pi * PB, std::false_type{});
+      else
+        pair(pg0, kb + 2 * pi * PB, vb + 2 * pi * PB, std::true_type{});
+    }
+  };
+  // the barrier in front of a stage waits for its loads and for the readers of the
+  // other set, which the next stage's loads then fill
+  const int nst = (npg + 7) >> 3;
+  dma(0, kl0, vl0);
+  for (int st = 0; st < nst; st += 2) {
+    __syncthreads();
+    if (st + 1 < nst) dma(st + 1, kl1, vl1);
+    __builtin_amdgcn_sched_barrier(0);
+    stage(st, kl0, vl0);
+    if (st + 1 < nst) {
+      __syncthreads();
+      if (st + 2 < nst) dma(st + 2, kl0, vl0);
+      __builtin_amdgcn_sched_barrier(0);
+      stage(st + 1, kl1, vl1);
+    }
+  }
+
+  // the KW shares of a row: sums scaled to the common maximum and added in order
+  if constexpr (KW > 1) {
+    __syncthreads();
+    constexpr int PER = 4 / RT;  // waves' accumulators (8 KB a tile) per 32 KB array
+    float4 *const area[4] = {(float4 *)kl0, (float4 *)vl0, (float4 *)kl1, (float4 *)vl1};
+    static_assert((KW - 1) * RW <= 4 * PER, "the stage buffers hold the shares");
+    if (kw > 0) {
+      const int w = (kw - 1) * RW + rw;
+      float4 *to = (w / PER == 0 ? area[0] : w / PER == 1 ? area[1] : w / PER == 2 ? area[2] : area[3]) + (w % PER) * (RT * 512);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          to[(rt * 8 + c) * 64 + lane] = make_float4(acc[rt][c][0], acc[rt][c][1], acc[rt][c][2], acc[rt][c][3]);
+    }
+    if (gq == 0)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        ms[kw][rw * RT + rt][r] = m_run[rt];
+        ls[kw][rw * RT + rt][r] = acc_l[rt][0];
+      }
+    __syncthreads();
+    if (kw > 0) return;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float mx = kNoScore;
+#pragma unroll
+      for (int k = 0; k < KW; ++k) mx = fmaxf(mx, ms[k][rw * RT + rt][r]);
+      const float f0 = __builtin_amdgcn_exp2f(m_run[rt] - mx);
+      m_run[rt] = mx;
+      acc_l[rt] = acc_l[rt] * f0;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) acc[rt][c] = acc[rt][c] * f0;
+#pragma unroll
+      for (int k = 1; k < KW; ++k) {
+        const int w = (k - 1) * RW + rw;
+        const float4 *from = (w / PER == 0 ? area[0] : w / PER == 1 ? area[1] : w / PER == 2 ? area[2] : area[3]) + (w % PER) * (RT * 512);
+        const float f = __builtin_amdgcn_exp2f(ms[k][rw * RT + rt][r] - mx);
+        acc_l[rt][0] += ls[k][rw * RT + rt][r] * f;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const float4 o = from[(rt * 8 + c) * 64 + lane];
+          acc[rt][c][0] += o.x * f;
+          acc[rt][c][1] += o.y * f;
+          acc[rt][c][2] += o.z * f;
+          acc[rt][c][3] += o.w * f;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int rho = wrow + rt * 16 + r;
+    if (rho >= rows) continue;
+    if (nsplit == 1) {
+      const float inv = 1.f / acc_l[rt][0];
+      uint16_t *o = (uint16_t *)a.O + place(rho) * DH + 4 * gq;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        *(u32x2 *)(o + 16 * c) = u32x2{pack2(acc[rt][c][0] * inv, acc[rt][c][1] * inv), pack2(acc[rt][c][2] * inv, acc[rt][c][3] * inv)};
+    } else {
+      const size_t at = ((size_t)a.s.part[i] + (size_t)split * rows + rho) * n_kv + g;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        *(float4 *)(a.opart + at * DH + 16 * c + 4 * gq) = make_float4(acc[rt][c][0], acc[rt][c][1], acc[rt][c][2], acc[rt][c][3]);
+      if (gq == 0) *(float2 *)(a.ostat + at * 2) = make_float2(m_run[rt], acc_l[rt][0]);
+    }
+  }
+}
+
+// fp32 cache: sixteen query rows of one (sequence, KV head) and a split of its
+// pages per workgroup, on the fp32 matrix instruction (attn_f32.h).
+template <int NC>
+__global__ __launch_bounds__(64 * kWavesF32Attn) void k_tree_attn_f32(TreeAttn a) {
+  const int i = blockIdx.z, g = blockIdx.y;
+  const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
+  const int G = a.n_q / a.kv.n_kv, rows = n * a.np * G, DH = a.kv.d_h;
+  const int blk = blockIdx.x / a.max_splits, split = blockIdx.x % a.max_splits;
+  const int npages = (len + 15) >> 4;
+  int each;
+  const int nsplit = tree_splits(npages, a.pages_per_split, &each);
+  if (blk * 16 >= rows || split >= nsplit) return;
+  const int pb = split * each, pe = min(npages, pb + each);
+  const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
+  __shared__ F32Merge<NC> mg;
+  __shared__ uint64_t line_s[kTreeNodes];
+  if (threadIdx.x < 64) line_s[threadIdx.x] = node_line(a.parents + first, n);
+  __syncthreads();
+  const int rho = blk * 16 + (threadIdx.x & 15);
+  const bool live = rho < rows;
+  const SeesLine sees{base, live ? line_s[rho / (G * a.np)] : 0};
+  attn_f32<NC>(mg, (const float *)a.Q + place(live ? rho : 0) * DH, live, sees, base >> 4, len, (const float *)a.kv.k,
+               (const float *)a.kv.v, a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps, pb, pe, a.kv.n_kv, g, DH);
+  for (int e = threadIdx.x; e < min(16, rows - blk * 16) * DH; e += 64 * kWavesF32Attn) {
+    const int qr = e / DH, dh = e % DH;
+    float o, l, mx;
+    mg.merged(qr, dh, o, l, mx);
+    if (nsplit == 1) {
+      ((float *)a.O)[place(blk * 16 + qr) * DH + dh] = o / l;
+    } else {
+      const size_t at = ((size_t)a.s.part[i] + (size_t)split * rows + blk * 16 + qr) * a.kv.n_kv + g;
+      a.opart[at * DH + dh] = o;
+      if (dh == 0) *(float2 *)(a.ostat + at * 2) = make_float2(mx, l);
+    }
+  }
+}
+
+// Splits of a sequence merged in split order: one thread per (query row, four
+// dimensions).
+template <typename T>
+__global__ __launch_bounds__(256) void k_tree_combine(TreeAttn a) {
+  const int i = blockIdx.z, g = blockIdx.y, DH = a.kv.d_h, Q4 = DH / 4;
+  const int first = a.s.off[i], n = a.s.off[i + 1] - first;
+  const int G = a.n_q / a.kv.n_kv, rows = n * a.np * G;
+  int each;
+  const int nsplit = tree_splits((a.s.base[i] + n + 15) >> 4, a.pages_per_split, &each);
+  const int e = blockIdx.x * 256 + threadIdx.x, rho = e / Q4, d4 = e % Q4;
+  if (nsplit == 1 || rho >= rows) return;
+  const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
+  const size_t at0 = ((size_t)a.s.part[i] + rho) * a.kv.n_kv + g, step = (size_t)rows * a.kv.n_kv;
+  float mx = kNoScore;
+#pragma unroll 8
+  for (int s = 0; s < nsplit; ++s) mx = fmaxf(mx, a.ostat[(at0 + s * step) * 2]);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float l = 0.f;
+#pragma unroll 8
+  for (int s = 0; s < nsplit; ++s) {
+    const size_t at = at0 + s * step;
+    const float2 ml = *(const float2 *)(a.ostat + at * 2);
+    const float f = exp2f(ml.x - mx);
+    const float4 v = ((const float4 *)(a.opart + at * DH))[d4];
+    o.x += v.x * f;
+    o.y += v.y * f;
+    o.z += v.z * f;
+    o.w += v.w * f;
+    l += ml.y * f;
+  }
+  T *out = (T *)a.O + place(rho) * DH + d4 * 4;
+  st<T>(out, 0, o.x / l);
+  st<T>(out, 1, o.y / l);
+  st<T>(out, 2, o.z / l);
+  st<T>(out, 3, o.w / l);
 }
 
 // The kept nodes' keys and values of one (layer, KV head, sequence): all read
@@ -105,15 +469,55 @@ hipError_t launch_tree_rows(const TreeSeqs &s, const int *parents, PromptRow *ro
   return hipGetLastError();
 }
 
+int tree_block_rows(int rows, int dtype) {
+  if (dtype != 1) return 16;
+  for (int r = 16; r < 256; r *= 2)
+    if (rows <= r) return r;
+  return 256;
+}
+
 hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st) {
-  if (a.kv.d_h > 128 || a.s.n < 1) return hipErrorInvalidValue;
-  const dim3 grid(a.max_nodes * a.np, a.n_q, a.s.n);
-  if (a.dtype == 1 && a.q32)
-    hipLaunchKernelGGL((k_tree_attn_simple<uint16_t, float>), grid, dim3(256), 0, st, a);
-  else if (a.dtype == 1)
-    hipLaunchKernelGGL((k_tree_attn_simple<uint16_t, uint16_t>), grid, dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((k_tree_attn_simple<float, float>), grid, dim3(256), 0, st, a);
+  const int rows = a.max_nodes * a.np * (a.n_q / a.kv.n_kv), cap = tree_block_rows(rows, a.dtype);
+  if (a.s.n < 1 || a.s.n > kTreeSeqs || a.max_nodes < 1 || a.max_nodes > kTreeNodes || a.max_splits < 1 || a.pages_per_split < 1 ||
+      a.pages_per_split + kTreeStagePages > kTreeMaxPages)  // (splits are rounded up to whole stages)
+    return hipErrorInvalidValue;
+  const dim3 grid((rows + cap - 1) / cap * a.max_splits, a.kv.n_kv, a.s.n);
+  if (a.dtype == 1) {
+    if (a.kv.d_h != 128) return hipErrorInvalidValue;
+    auto go = [&](auto q) {
+      typedef decltype(q) QT;
+      switch (cap) {
+        case 16: hipLaunchKernelGGL((k_tree_attn_bf16<1, 1, 4, QT>), grid, dim3(256), 0, st, a); break;
+        case 32: hipLaunchKernelGGL((k_tree_attn_bf16<2, 1, 4, QT>), grid, dim3(256), 0, st, a); break;
+        case 64: hipLaunchKernelGGL((k_tree_attn_bf16<2, 2, 4, QT>), grid, dim3(512), 0, st, a); break;
+        case 128: hipLaunchKernelGGL((k_tree_attn_bf16<2, 4, 2, QT>), grid, dim3(512), 0, st, a); break;
+        default: hipLaunchKernelGGL((k_tree_attn_bf16<2, 8, 1, QT>), grid, dim3(512), 0, st, a); break;
+      }
+    };
+    if (a.q32) go(float{});
+    else go(uint16_t{});
+  } else {
+    if (a.kv.d_h > 128) return hipErrorInvalidValue;
+    const dim3 block(64 * kWavesF32Attn);
+    switch ((a.kv.d_h + 15) / 16) {
+      case 1: hipLaunchKernelGGL(k_tree_attn_f32<1>, grid, block, 0, st, a); break;
+      case 2: hipLaunchKernelGGL(k_tree_attn_f32<2>, grid, block, 0, st, a); break;
+      case 3: hipLaunchKernelGGL(k_tree_attn_f32<3>, grid, block, 0, st, a); break;
+      case 4: hipLaunchKernelGGL(k_tree_attn_f32<4>, grid, block, 0, st, a); break;
+      case 5: hipLaunchKernelGGL(k_tree_attn_f32<5>, grid, block, 0, st, a); break;
+      case 6: hipLaunchKernelGGL(k_tree_attn_f32<6>, grid, block, 0, st, a); break;
+      case 7: hipLaunchKernelGGL(k_tree_attn_f32<7>, grid, block, 0, st, a); break;
+      default: hipLaunchKernelGGL(k_tree_attn_f32<8>, grid, block, 0, st, a); break;
+    }
+  }
+  if (const hipError_t e = hipGetLastError()) return e;
+  if (a.max_splits > 1) {
+    const dim3 cgrid((rows * (a.kv.d_h / 4) + 255) / 256, a.kv.n_kv, a.s.n);
+    if (a.dtype == 1)
+      hipLaunchKernelGGL(k_tree_combine<uint16_t>, cgrid, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL(k_tree_combine<float>, cgrid, dim3(256), 0, st, a);
+  }
   return hipGetLastError();
 }
 
