@@ -159,6 +159,7 @@ k_tree_attn_bf16(TreeAttn a) {
   const int kpage = r >> 3, kpos = 8 * ((r >> 2) & 1) + (r & 3);
   const int vpage = gq >> 1, vpos = 8 * (gq & 1);
   const bool active = wrow < rows;
+  bool odd = false;  // some node's value is not finite
 
   auto pair = [&](int pg0, const uint16_t *kb, const uint16_t *vb, auto masked) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
@@ -184,22 +185,20 @@ k_tree_attn_bf16(TreeAttn a) {
     for (int c = 0; c < 8; ++c) vf[c] = *(const u32x4 *)&vb[(vpage * DH + c * 16 + r) * 16 + vpos];
     const int kp0 = (pb + pg0 + vpage) * 16 + vpos;  // position of this lane's first score
     const bool page_ok = pg0 + vpage < npg;
-    bool odd = false;
     if (MASKED) {
-      // slots past the sequence may hold anything; values of nodes that are
-      // not finite would reach the rows that do not see them as 0 * infinity,
-      // so they are taken out here and added below
+      // slots past the sequence may hold anything; a node's values that are not
+      // finite would reach the rows that do not see it as 0 * infinity, so
+      // they are taken out here and added at the end
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         vf[c] = mask8(vf[c], kp0, page_ok ? len : kp0);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          uint32_t x = vf[c][w];
-          const bool lo = (x & 0x7f80u) == 0x7f80u, hi = (x & 0x7f800000u) == 0x7f800000u;
-          if (lo) x &= 0xffff0000u;
-          if (hi) x &= 0x0000ffffu;
+          const uint32_t x = vf[c][w];
+          const bool lo = (x & 0x7f80u) == 0x7f80u && kp0 + 2 * w >= base;
+          const bool hi = (x & 0x7f800000u) == 0x7f800000u && kp0 + 2 * w + 1 >= base;
           odd |= lo | hi;
-          vf[c][w] = x;
+          vf[c][w] = x & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
         }
       }
     }
@@ -248,54 +247,59 @@ k_tree_attn_bf16(TreeAttn a) {
       for (int c = 0; c < 8; ++c)
         acc[rt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[c]),
                                                              __builtin_bit_cast(bf16x8, pf), acc[rt][c], 0, 0, 0);
-      if (MASKED && __any(odd)) {
-        // key by key: lane r + 16 h holds row r's probabilities of group h's positions
-#pragma unroll 1
-        for (int h = 0; h < 4; ++h)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float pk = __shfl(p[e], r + 16 * h, 64);
-            const bool sees = (__shfl(seen, r + 16 * h, 64) >> e) & 1;
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-#pragma unroll
-              for (int d = 0; d < 4; ++d) {
-                const uint16_t x = vb[((h >> 1) * DH + 16 * c + 4 * gq + d) * 16 + 8 * (h & 1) + e];
-                if (sees && (x & 0x7f80) == 0x7f80) acc[rt][c][d] += pk * bf2f(x);
-              }
-          }
-      }
     }
   };
-  auto stage = [&](int st, const uint16_t *kb, const uint16_t *vb) __attribute__((always_inline)) {
+  auto stage = [&](int st, const uint16_t *kb, const uint16_t *vb, auto masked) __attribute__((always_inline)) {
     if (!active) return;
-#pragma unroll
+#pragma unroll 1
     for (int j = 0; j < PP; ++j) {
       const int pi = kw * PP + j, pg0 = st * 8 + 2 * pi;
-      if (pg0 >= npg) break;
-      if ((pb + pg0 + 2) * 16 <= base && pg0 + 2 <= npg)
-        pair(pg0, kb + 2 * pi * PB, vb + 2 * pi * PB, std::false_type{});
-      else
-        pair(pg0, kb + 2 * pi * PB, vb + 2 * pi * PB, std::true_type{});
+      if (decltype(masked)::value && pg0 >= npg) break;
+      pair(pg0, kb + 2 * pi * PB, vb + 2 * pi * PB, masked);
     }
   };
-  // the barrier in front of a stage waits for its loads and for the readers of the
-  // other set, which the next stage's loads then fill
-  const int nst = (npg + 7) >> 3;
+  // The barrier in front of a stage waits for its loads and for the readers of
+  // the other set, which the next stage's loads then fill.  Stages of which
+  // every row sees every key first, in pairs so that each set is known; then
+  // the last ones, up to two but for a split that ends inside a stage.
+  const int nst = (npg + 7) >> 3, nfull = max(0, min(npg, (base >> 4) - pb)) >> 3;
   dma(0, kl0, vl0);
-  for (int st = 0; st < nst; st += 2) {
+  for (int st = 0; st < nfull; st += 2) {
     __syncthreads();
     if (st + 1 < nst) dma(st + 1, kl1, vl1);
     __builtin_amdgcn_sched_barrier(0);
-    stage(st, kl0, vl0);
-    if (st + 1 < nst) {
+    stage(st, kl0, vl0, std::false_type{});
+    if (st + 1 < nfull) {
       __syncthreads();
       if (st + 2 < nst) dma(st + 2, kl0, vl0);
       __builtin_amdgcn_sched_barrier(0);
-      stage(st + 1, kl1, vl1);
+      stage(st + 1, kl1, vl1, std::false_type{});
     }
   }
+#pragma unroll 1
+  for (int st = nfull; st < nst; ++st) {
+    __syncthreads();
+    const bool set1 = st & 1;
+    if (st + 1 < nst) dma(st + 1, set1 ? kl0 : kl1, set1 ? vl0 : vl1);
+    stage(st, set1 ? kl1 : kl0, set1 ? vl1 : vl0, std::true_type{});
+  }
 
+  if (__any(odd)) {
+    // such values make the sums of the rows that see them infinite or NaN,
+    // whatever their weights
+    for (int pos = max(base, pb * 16); pos < min(len, (pb + npg) * 16); ++pos) {
+      const uint16_t *v = vbase + ((size_t)ptab[(pos >> 4) - pb] * n_kv + g) * PB + (pos & 15);
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const uint16_t x = v[(16 * c + 4 * gq + d) * 16];
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+            if ((x & 0x7f80) == 0x7f80 && ((line[rt] >> (pos - base)) & 1)) acc[rt][c][d] += bf2f(x);
+        }
+    }
+  }
   // the KW shares of a row: sums scaled to the common maximum and added in order
   if constexpr (KW > 1) {
     __syncthreads();
