@@ -484,12 +484,12 @@ dbt_status flush(dbt_kv *kv, const int *h_pos, int npos, hipStream_t st, StepBeg
   return DBT_OK;
 }
 
-// A tree call's sequences in launches of up to kTreeSeqs, how its attention
-// splits the cache, and its workspace.
+// A tree call's sequences in launches of up to kTreeSeqs, its blocks of query rows
+// and its workspace.
 struct TreePlan {
   std::vector<TreeSeqs> groups;
   const int *parents = nullptr;
-  int nodes = 0, max_nodes = 0, pages_per_split = 1, max_splits = 1;
+  int nodes = 0, max_nodes = 0, block = 0;
   float *opart = nullptr, *ostat = nullptr;
   PromptRow *map = nullptr;
 };
@@ -514,9 +514,8 @@ struct LayerCall {
 
 hipError_t tree_attn(const TreePlan &t, TreeAttn a, hipStream_t st) {
   a.parents = t.parents;
-  a.pages_per_split = t.pages_per_split;
-  a.max_splits = t.max_splits;
   a.max_nodes = t.max_nodes;
+  a.block = t.block;
   a.opart = t.opart;
   a.ostat = t.ostat;
   for (const TreeSeqs &s : t.groups) {
@@ -1365,13 +1364,11 @@ dbt_status decode_step_impl(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, int
 
 // ---- drafted tokens ----
 
-// How a tree's attention splits the cache (plan_tree).  A workgroup fills a
-// compute unit (its stages take most of the LDS), so a call runs in rounds of
-// kComputeUnits workgroups.  In pages of reading time: a workgroup's start, and
-// the merge of the splits (a launch, and each row's partial result written and read).
-constexpr int kTreeMinPages = 2 * kTreeStagePages, kTreeMostPages = kTreeMaxPages - kTreeStagePages;
-constexpr int kTreeRounds = 4, kTreeStart = 6, kTreeMerge = 14, kTreeMergeRows = 8;
-constexpr int kTreeRows = 256;  // query rows of one workgroup, at most
+// How a tree's attention cuts its work (plan_tree).  A workgroup fills a compute
+// unit (its stages take most of the LDS).  In pages of reading time (8 KB of keys
+// and values each): a piece's start, the merge's launch, and kTreeMergeRows rows' partial
+// results written and read (512 bytes each way).
+constexpr int kTreeStart = 6, kTreeMerge = 14, kTreeMergeRows = 8;
 
 // may_be_empty: calls without a launch over the nodes
 dbt_status check_tree(const dbt_kv *kv, const dbt_tree *t, int *nodes, bool may_be_empty = false) {
@@ -1427,101 +1424,65 @@ void give_back_pages(dbt_kv *kv, int b, size_t keep) {
                     kv->pending.end());
 }
 
-// Rows of partial results (of every KV head) that a call over up to `nodes`
-// nodes and `pages` pages a sequence can need: splits are chosen for at most
-// kTreeRounds rounds, or are as long as they may be.
-size_t tree_partial_rows(const dbt_config &c, int nodes, int pages) {
-  const size_t rows = (size_t)nodes * (1 + n_branches(c)) * c.n_q_heads;
-  const size_t rounds = (size_t)kTreeRounds * kComputeUnits * kTreeRows;
-  return std::min(rows * ((pages + kTreeMinPages - 1) / kTreeMinPages),
-                  std::max(rounds, rows * ((pages + kTreeMostPages - 1) / kTreeMostPages)));
-}
-
 struct TreeLayout {
   size_t map, opart, ostat, total;
 };
 TreeLayout tree_layout(const dbt_config &c, int nodes) {
   TreeLayout L;
-  const int pages = (c.max_pos + kPage - 1) / kPage;
-  const size_t rows = pages > kTreeMinPages ? tree_partial_rows(c, nodes, pages) : 0;
+  // cut units leave two pieces a workgroup at most
+  const int rows = std::min(nodes, DBT_TREE_NODES) * (1 + n_branches(c)) * (c.n_q_heads / c.n_kv_heads);
+  const size_t slots = (size_t)2 * kComputeUnits * tree_block_rows(rows, c.dtype);
   L.map = 0;
   L.opart = align256((size_t)nodes * sizeof(PromptRow));
-  L.ostat = L.opart + align256(rows * c.head_dim * 4);
-  L.total = L.ostat + align256(rows * 2 * 4);
+  L.ostat = L.opart + align256(slots * c.head_dim * 4);
+  L.total = L.ostat + align256(slots * 2 * 4);
   return L;
 }
 
-// Pages per split of a tree call.  Equal splits in as few rounds as they fit,
-// by the estimate above; sequences as long as each other and enough of them
-// are not split.  32 sequences of 4096 positions and 8 KV heads, 64 rows each: one
-// workgroup for each of the 256 (sequence, KV head).
-int tree_pages_per_split(const dbt_config &c, const dbt_tree *t, int n_paths, const int *base) {
+// The schedule of up to kTreeSeqs sequences (see TreeSeqs): whole units, or equal
+// runs for kComputeUnits workgroups, whichever the estimate above makes shorter.
+void schedule_tree(const dbt_config &c, int n_paths, int block, TreeSeqs *g) {
   const int G = c.n_q_heads / c.n_kv_heads;
-  struct Seq { int pages, units; };
-  std::vector<Seq> seqs;
-  int longest = 1, most = 0;
-  long long total = 0, units = 0;
-  for (int b = 0; b < t->batch; ++b) most = std::max(most, t->h_nodes[b]);
-  const int rows = most * n_paths * G, cap = tree_block_rows(rows, c.dtype);
-  for (int b = 0; b < t->batch; ++b) {
-    const int n = t->h_nodes[b];
-    if (n == 0) continue;
-    const Seq s{(base[b] + n + kPage - 1) / kPage, c.n_kv_heads * ((n * n_paths * G + cap - 1) / cap)};
-    seqs.push_back(s);
-    longest = std::max(longest, s.pages);
-    total += (long long)s.pages * s.units;
-    units += s.units;
-  }
-  auto workgroups = [&](int target) {
-    long long w = 0;
-    int each;
-    for (const Seq &s : seqs) w += (long long)s.units * tree_splits(s.pages, target, &each);
-    return w;
+  long long units = 0, total = 0;
+  int longest = 0;
+  auto stages = [&](int i) {
+    const int pages = (g->base[i] + g->off[i + 1] - g->off[i] + kPage - 1) / kPage;
+    return (pages + kTreeStagePages - 1) / kTreeStagePages;
   };
-  // unsplit: the longest sequence, or the rounds of the average one
-  const int whole = std::min(longest, kTreeMostPages);
-  const long long avg = units ? total / units : 0;
-  long long best = std::max<long long>(longest + kTreeStart,
-                                       (workgroups(whole) + kComputeUnits - 1) / kComputeUnits * (avg + kTreeStart));
-  int choice = whole;
-  for (int k = 1; k <= kTreeRounds; ++k) {
-    int lo = kTreeMinPages / kTreeStagePages, hi = (whole + kTreeStagePages - 1) / kTreeStagePages;
-    if (hi * kTreeStagePages > kTreeMostPages) hi = kTreeMostPages / kTreeStagePages;
-    if (lo >= hi || workgroups(hi * kTreeStagePages) > (long long)k * kComputeUnits) continue;
-    while (lo < hi) {  // the shortest splits that fit k rounds
-      const int mid = (lo + hi) / 2;
-      if (workgroups(mid * kTreeStagePages) <= (long long)k * kComputeUnits) hi = mid;
-      else lo = mid + 1;
-    }
-    const int target = lo * kTreeStagePages;
-    if (target >= whole) continue;
-    const long long cost = (long long)k * (target + kTreeStart) + kTreeMerge + std::min(rows, cap) / kTreeMergeRows;
-    if (cost < best) {
-      best = cost;
-      choice = target;
-    }
+  auto of_seq = [&](int i) {
+    return (long long)c.n_kv_heads * (((g->off[i + 1] - g->off[i]) * n_paths * G + block - 1) / block);
+  };
+  for (int i = 0; i < g->n; ++i) {
+    units += of_seq(i);
+    total += of_seq(i) * stages(i);
+    longest = std::max(longest, stages(i));
   }
-  return choice;
+  const long long rounds = (units + kComputeUnits - 1) / kComputeUnits, run = (total + kComputeUnits - 1) / kComputeUnits;
+  const long long P = kTreeStagePages;
+  const long long whole = (units <= kComputeUnits ? longest * P : std::max(longest * P, run * P + longest * P / 2)) + rounds * kTreeStart;
+  const long long cut = run * P + 2 * (kTreeStart + block / kTreeMergeRows) + kTreeMerge;
+  g->whole = whole <= cut;
+  g->per = g->whole ? 1 : (int)run;
+  g->first[0] = 0;
+  for (int i = 0; i < g->n; ++i) g->first[i + 1] = g->first[i] + (int)of_seq(i) * (g->whole ? 1 : stages(i));
 }
 
 // base[b]: positions of sequence b before its nodes.
-dbt_status plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths, const int *base, char *ws, TreePlan *out) {
+TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths, const int *base, char *ws) {
   const dbt_config &cf = m->cfg;
-  TreePlan &p = *out;
+  TreePlan p;
   p.parents = t->parents;
   p.nodes = nodes;
   const TreeLayout L = tree_layout(cf, nodes);
   p.map = (PromptRow *)(ws + L.map);
   p.opart = (float *)(ws + L.opart);
   p.ostat = (float *)(ws + L.ostat);
-  const int G = cf.n_q_heads / cf.n_kv_heads;
-  p.pages_per_split = tree_pages_per_split(cf, t, n_paths, base);
+  for (int b = 0; b < t->batch; ++b) p.max_nodes = std::max(p.max_nodes, t->h_nodes[b]);
+  p.block = tree_block_rows(p.max_nodes * n_paths * (cf.n_q_heads / cf.n_kv_heads), cf.dtype);
   int off = 0;
-  long long part = 0;
   for (int b = 0; b < t->batch; ++b) {
     const int n = t->h_nodes[b];
     if (n == 0) continue;
-    p.max_nodes = std::max(p.max_nodes, n);
     if (p.groups.empty() || p.groups.back().n == kTreeSeqs) {
       p.groups.emplace_back();
       p.groups.back().n = 0;
@@ -1530,16 +1491,11 @@ dbt_status plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_pat
     TreeSeqs &g = p.groups.back();
     g.seq[g.n] = b;
     g.base[g.n] = base[b];
-    g.part[g.n] = (int)part;
     off += n;
-    int each;
-    const int ns = tree_splits((base[b] + n + kPage - 1) / kPage, p.pages_per_split, &each);
-    p.max_splits = std::max(p.max_splits, ns);
-    if (ns > 1) part += (long long)ns * n * n_paths * G;
     g.off[++g.n] = off;
   }
-  if (part > 0 && (size_t)part * cf.n_kv_heads * 2 * 4 > L.total - L.ostat) return fail(DBT_ERR_STATE, "internal: tree partials");
-  return DBT_OK;
+  for (TreeSeqs &g : p.groups) schedule_tree(cf, n_paths, p.block, &g);
+  return p;
 }
 
 }  // namespace
@@ -1915,8 +1871,7 @@ dbt_status dbt_tree_attention(dbt_kv *kv, int32_t layer, const dbt_tree *tree, i
     base[b] = kv->len[b] - tree->h_nodes[b];
     if (base[b] < 0) return fail(DBT_ERR_ARG, "sequence %d has %d positions and %d nodes", b, kv->len[b], tree->h_nodes[b]);
   }
-  TreePlan plan;
-  if ((s = plan_tree(kv->m, tree, nodes, n_paths, base.data(), (char *)workspace, &plan))) return s;
+  const TreePlan plan = plan_tree(kv->m, tree, nodes, n_paths, base.data(), (char *)workspace);
   hipStream_t st = (hipStream_t)stream;
   if ((s = flush(kv, nullptr, 0, st))) return s;
   TreeAttn a{};
@@ -1955,8 +1910,7 @@ dbt_status dbt_decode_tree(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, cons
   if ((s = check_tree_growth(kv, tree))) return s;
   const int nb = n_branches(cf), R = nodes, Rp = round16(nodes);
   const Rows rows{R, Rp, 0, on ? 1 + nb : 1};
-  TreePlan plan;
-  if ((s = plan_tree(m, tree, nodes, cf.compute_matched ? 1 : rows.np, kv->len.data(), (char *)workspace, &plan))) return s;
+  const TreePlan plan = plan_tree(m, tree, nodes, cf.compute_matched ? 1 : rows.np, kv->len.data(), (char *)workspace);
   hipStream_t st = (hipStream_t)stream;
   if ((s = ensure_device(m, st))) return s;  // before any state changes
   m->bnd_kv = nullptr;

@@ -354,13 +354,20 @@ hipError_t launch_attn_prefill(const PromptAttn &a, hipStream_t st);
 
 // ---- drafted tokens (tree_attention.hip) ----
 // Sequences of a tree call that have nodes: sequence seq[i] has base[i]
-// positions before its nodes, which are rows off[i] .. off[i + 1] - 1 of the
-// call; its partial results start at row part[i] (per KV head, split and query row).
+// positions before its nodes, which are rows off[i] .. off[i + 1] - 1 of the call.
+//
+// The attention's work is units of one (sequence, KV head, block of query
+// rows), sequence by sequence, blocks next to each other; a unit is its pages in
+// stages of kTreeStagePages.  Either every workgroup takes a whole unit
+// (whole), or all of them equal runs of `per` stages of the units in a row, so
+// that units are cut where runs end; first[i] counts the units (whole) or
+// stages before those of sequence i.
 constexpr int kTreeSeqs = 128;
 constexpr int kTreeNodes = 64;  // DBT_TREE_NODES: one lane, one bit of a line of ancestors each
+constexpr int kTreeStagePages = 8;
 struct TreeSeqs {
-  int n;
-  int seq[kTreeSeqs], base[kTreeSeqs], off[kTreeSeqs + 1], part[kTreeSeqs];
+  int n, whole, per;
+  int seq[kTreeSeqs], base[kTreeSeqs], off[kTreeSeqs + 1], first[kTreeSeqs + 1];
 };
 // Row map of the nodes (position, sequence, slot; kept nowhere).
 hipError_t launch_tree_rows(const TreeSeqs &s, const int *parents, PromptRow *rows, hipStream_t st);
@@ -374,26 +381,14 @@ struct TreeAttn {
   KVRef kv;
   int n_q, np;        // query heads, paths
   int dtype;
-  int pages_per_split;  // see tree_splits
-  int max_splits;
-  int max_nodes;      // of one sequence
-  float *opart;       // [partial row][n_kv][d_h]
-  float *ostat;       // [partial row][n_kv][2]
+  int max_nodes;      // of one sequence of the call
+  int block;          // tree_block_rows of it
+  float *opart;       // [2 * workgroups][block][d_h]: the pieces of units cut by runs
+  float *ostat;       // [2 * workgroups][block][2]
 };
 hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st);
-// Splits a sequence of `pages` pages is read in and the pages of each (the last
-// may be shorter): about equal, and whole stages of the kernel.
-constexpr int kTreeStagePages = 8;
-constexpr int kTreeMaxPages = 1024;  // pages of one split (their ids are kept in LDS)
-#ifdef __HIPCC__
-__host__ __device__
-#endif
-inline int tree_splits(int pages, int pages_per_split, int *each) {
-  const int n = (pages + pages_per_split - 1) / pages_per_split;
-  *each = n <= 1 ? pages : ((pages + n - 1) / n + kTreeStagePages - 1) / kTreeStagePages * kTreeStagePages;
-  return n <= 1 ? 1 : (pages + *each - 1) / *each;
-}
-// Query rows (nodes x paths x query heads of a KV head) of one workgroup.
+// Query rows of one unit, at most, where a sequence has up to `rows` for a KV head
+// (nodes x paths x query heads of the KV head).
 int tree_block_rows(int rows, int dtype);
 // Kept nodes of up to kKeepSeqs sequences: node path[i][j] of sequence seq[i]
 // moves to position base[i] + j, j = first[i] .. count[i] - 1 (those before

@@ -47,7 +47,51 @@ struct RowPlace {
   }
 };
 
+// The next piece of work of workgroup w at position s of the schedule
+// (TreeSeqs): stages st0 .. st1 - 1 of unit (sequence i, KV head g, block blk),
+// which has `stages` of them.
+struct Piece {
+  int i, g, blk, st0, st1, stages;
+  __device__ __forceinline__ bool is_whole() const { return st0 == 0 && st1 == stages; }
+  // A workgroup has at most one piece that begins inside a unit (its first)
+  // and one that begins a unit without ending it (its last).
+  __device__ __forceinline__ int slot(int w) const { return 2 * w + (st0 == 0); }
+};
+__device__ __forceinline__ int seq_rows(const TreeAttn &a, int i) {
+  return (a.s.off[i + 1] - a.s.off[i]) * a.np * (a.n_q / a.kv.n_kv);
+}
+__device__ __forceinline__ int seq_stages(const TreeAttn &a, int i) {
+  const int pages = (a.s.base[i] + a.s.off[i + 1] - a.s.off[i] + 15) >> 4;
+  return (pages + kTreeStagePages - 1) / kTreeStagePages;
+}
+__device__ __forceinline__ Piece piece_at(const TreeAttn &a, int s, int end) {
+  int lo = 0, hi = a.s.n;  // first[lo] <= s < first[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (a.s.first[mid] <= s) lo = mid;
+    else hi = mid;
+  }
+  Piece p;
+  p.i = lo;
+  p.stages = seq_stages(a, lo);
+  const int len = a.s.whole ? 1 : p.stages, rem = s - a.s.first[lo], unit = rem / len;
+  const int nblk = (seq_rows(a, lo) + a.block - 1) / a.block;
+  p.blk = unit % nblk;
+  p.g = unit / nblk;
+  p.st0 = a.s.whole ? 0 : rem % len;
+  p.st1 = a.s.whole ? p.stages : min(p.stages, p.st0 + end - s);
+  return p;
+}
+// Workgroups are dealt to the eight XCDs in turn: workgroup b takes a place that
+// keeps neighbours of the schedule (blocks of one (sequence, KV head), which
+// read the same pages) on one XCD and its L2.
+__device__ __forceinline__ int schedule_place(int b, int n) {
+  const int x = b & 7, q = n >> 3, r = n & 7;
+  return x * q + min(x, r) + (b >> 3);
+}
+
 typedef __attribute__((address_space(3))) void lds_void;
+constexpr int kWindow = 128;  // stages whose page ids are in LDS together
 
 // Growth of a row's score maximum (base 2) that moves its softmax base.
 constexpr float kLazyMargin = 8.f;
@@ -75,27 +119,25 @@ k_tree_attn_bf16(TreeAttn a) {
   // two sets of stage buffers, separate arrays so that the loads filling one
   // set are told apart from the reads of the other
   __shared__ __attribute__((aligned(16))) uint16_t kl0[8 * PB], vl0[8 * PB], kl1[8 * PB], vl1[8 * PB];
-  __shared__ int pid_s[kTreeMaxPages];
+  __shared__ int pid_s[kWindow * kTreeStagePages];
   __shared__ uint64_t line_s[kTreeNodes];
   __shared__ float ms[KW][RW * RT][16], ls[KW][RW * RT][16];
-  const int i = blockIdx.z, g = blockIdx.y;
-  const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
-  const int G = a.n_q / a.kv.n_kv, rows = n * a.np * G;
-  const int blk = blockIdx.x / a.max_splits, split = blockIdx.x % a.max_splits;
-  const int row0 = blk * (RW * RT * 16);
-  const int npages = (len + 15) >> 4;
-  int each;
-  const int nsplit = tree_splits(npages, a.pages_per_split, &each);
-  if (row0 >= rows || split >= nsplit) return;
-  const int pb = split * each, npg = min(npages, pb + each) - pb;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int rw = wave % RW, kw = wave / RW;
   const int r = lane & 15, gq = lane >> 4;
-  const int n_kv = a.kv.n_kv;
-  const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
+  const int n_kv = a.kv.n_kv, G = a.n_q / n_kv;
   const float scale = kLog2e / sqrtf((float)DH);
-  const int *ptab = a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps + pb;
-  for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[k];
+  const int w = schedule_place(blockIdx.x, gridDim.x), end = min(a.s.first[a.s.n], (w + 1) * a.s.per);
+  for (int at = w * a.s.per; at < end;) {
+  const Piece pc = piece_at(a, at, end);
+  at += a.s.whole ? 1 : pc.st1 - pc.st0;
+  const int i = pc.i, g = pc.g;
+  const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
+  const int rows = n * a.np * G, row0 = pc.blk * (RW * RT * 16);
+  const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
+  const int *ptab = a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps;
+  const int pages0 = pc.st0 * 8, pages1 = min((len + 15) >> 4, pc.st1 * 8);  // the piece's pages
+  __syncthreads();  // (the last piece's readers)
   if (wave == 0) line_s[lane] = node_line(a.parents + first, n);
   __syncthreads();
 
@@ -125,6 +167,7 @@ k_tree_attn_bf16(TreeAttn a) {
   // without bank conflicts.  V rows (one dimension, 32 bytes) need no swizzle.
   auto kswz = [](int row) { return ((row & 3) | ((row >> 3) << 2)) << 1; };
   const uint16_t *kbase = (const uint16_t *)a.kv.k, *vbase = (const uint16_t *)a.kv.v;
+  int pb = 0, npg = 0;  // the window's first page, its pages
   // A stage is 64 loads of 1 KB, four of K and four of V a page: each wave takes
   // 64 / NW.  Pages past the split's last re-read it (never used unmasked).
   auto dma = [&](int st, uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
@@ -261,34 +304,40 @@ k_tree_attn_bf16(TreeAttn a) {
   // The barrier in front of a stage waits for its loads and for the readers of
   // the other set, which the next stage's loads then fill.  Stages of which
   // every row sees every key first, in pairs so that each set is known; then
-  // the last ones, up to two but for a split that ends inside a stage.
-  const int nst = (npg + 7) >> 3, nfull = max(0, min(npg, (base >> 4) - pb)) >> 3;
-  dma(0, kl0, vl0);
-  for (int st = 0; st < nfull; st += 2) {
+  // the last ones, those from the page of position `base` on.
+  for (pb = pages0; pb < pages1; pb += kWindow * 8) {
+    npg = min(pages1 - pb, kWindow * 8);
     __syncthreads();
-    if (st + 1 < nst) dma(st + 1, kl1, vl1);
-    __builtin_amdgcn_sched_barrier(0);
-    stage(st, kl0, vl0, std::false_type{});
-    if (st + 1 < nfull) {
+    for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
+    __syncthreads();
+    const int nst = (npg + 7) >> 3, nfull = max(0, min(npg, (base >> 4) - pb)) >> 3;
+    dma(0, kl0, vl0);
+    for (int st = 0; st < nfull; st += 2) {
       __syncthreads();
-      if (st + 2 < nst) dma(st + 2, kl0, vl0);
+      if (st + 1 < nst) dma(st + 1, kl1, vl1);
       __builtin_amdgcn_sched_barrier(0);
-      stage(st + 1, kl1, vl1, std::false_type{});
+      stage(st, kl0, vl0, std::false_type{});
+      if (st + 1 < nfull) {
+        __syncthreads();
+        if (st + 2 < nst) dma(st + 2, kl0, vl0);
+        __builtin_amdgcn_sched_barrier(0);
+        stage(st + 1, kl1, vl1, std::false_type{});
+      }
     }
-  }
 #pragma unroll 1
-  for (int st = nfull; st < nst; ++st) {
-    __syncthreads();
-    const bool set1 = st & 1;
-    if (st + 1 < nst) dma(st + 1, set1 ? kl0 : kl1, set1 ? vl0 : vl1);
-    stage(st, set1 ? kl1 : kl0, set1 ? vl1 : vl0, std::true_type{});
+    for (int st = nfull; st < nst; ++st) {
+      __syncthreads();
+      const bool set1 = st & 1;
+      if (st + 1 < nst) dma(st + 1, set1 ? kl0 : kl1, set1 ? vl0 : vl1);
+      stage(st, set1 ? kl1 : kl0, set1 ? vl1 : vl0, std::true_type{});
+    }
   }
 
   if (__any(odd)) {
     // such values make the sums of the rows that see them infinite or NaN,
     // whatever their weights
-    for (int pos = max(base, pb * 16); pos < min(len, (pb + npg) * 16); ++pos) {
-      const uint16_t *v = vbase + ((size_t)ptab[(pos >> 4) - pb] * n_kv + g) * PB + (pos & 15);
+    for (int pos = max(base, pages0 * 16); pos < min(len, pages1 * 16); ++pos) {
+      const uint16_t *v = vbase + ((size_t)ptab[pos >> 4] * n_kv + g) * PB + (pos & 15);
 #pragma unroll
       for (int c = 0; c < 8; ++c)
 #pragma unroll
@@ -307,8 +356,8 @@ k_tree_attn_bf16(TreeAttn a) {
     float4 *const area[4] = {(float4 *)kl0, (float4 *)vl0, (float4 *)kl1, (float4 *)vl1};
     static_assert((KW - 1) * RW <= 4 * PER, "the stage buffers hold the shares");
     if (kw > 0) {
-      const int w = (kw - 1) * RW + rw;
-      float4 *to = (w / PER == 0 ? area[0] : w / PER == 1 ? area[1] : w / PER == 2 ? area[2] : area[3]) + (w % PER) * (RT * 512);
+      const int k = (kw - 1) * RW + rw;
+      float4 *to = (k / PER == 0 ? area[0] : k / PER == 1 ? area[1] : k / PER == 2 ? area[2] : area[3]) + (k % PER) * (RT * 512);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -322,7 +371,7 @@ k_tree_attn_bf16(TreeAttn a) {
         ls[kw][rw * RT + rt][r] = acc_l[rt][0];
       }
     __syncthreads();
-    if (kw > 0) return;
+    if (kw > 0) continue;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       float mx = kNoScore;
@@ -335,8 +384,8 @@ k_tree_attn_bf16(TreeAttn a) {
       for (int c = 0; c < 8; ++c) acc[rt][c] = acc[rt][c] * f0;
 #pragma unroll
       for (int k = 1; k < KW; ++k) {
-        const int w = (k - 1) * RW + rw;
-        const float4 *from = (w / PER == 0 ? area[0] : w / PER == 1 ? area[1] : w / PER == 2 ? area[2] : area[3]) + (w % PER) * (RT * 512);
+        const int q = (k - 1) * RW + rw;
+        const float4 *from = (q / PER == 0 ? area[0] : q / PER == 1 ? area[1] : q / PER == 2 ? area[2] : area[3]) + (q % PER) * (RT * 512);
         const float f = __builtin_amdgcn_exp2f(ms[k][rw * RT + rt][r] - mx);
         acc_l[rt][0] += ls[k][rw * RT + rt][r] * f;
 #pragma unroll
@@ -354,83 +403,86 @@ k_tree_attn_bf16(TreeAttn a) {
   for (int rt = 0; rt < RT; ++rt) {
     const int rho = wrow + rt * 16 + r;
     if (rho >= rows) continue;
-    if (nsplit == 1) {
+    if (pc.is_whole()) {
       const float inv = 1.f / acc_l[rt][0];
       uint16_t *o = (uint16_t *)a.O + place(rho) * DH + 4 * gq;
 #pragma unroll
       for (int c = 0; c < 8; ++c)
         *(u32x2 *)(o + 16 * c) = u32x2{pack2(acc[rt][c][0] * inv, acc[rt][c][1] * inv), pack2(acc[rt][c][2] * inv, acc[rt][c][3] * inv)};
     } else {
-      const size_t at = ((size_t)a.s.part[i] + (size_t)split * rows + rho) * n_kv + g;
+      const size_t to = (size_t)pc.slot(w) * a.block + rho - row0;
 #pragma unroll
       for (int c = 0; c < 8; ++c)
-        *(float4 *)(a.opart + at * DH + 16 * c + 4 * gq) = make_float4(acc[rt][c][0], acc[rt][c][1], acc[rt][c][2], acc[rt][c][3]);
-      if (gq == 0) *(float2 *)(a.ostat + at * 2) = make_float2(m_run[rt], acc_l[rt][0]);
+        *(float4 *)(a.opart + to * DH + 16 * c + 4 * gq) = make_float4(acc[rt][c][0], acc[rt][c][1], acc[rt][c][2], acc[rt][c][3]);
+      if (gq == 0) *(float2 *)(a.ostat + to * 2) = make_float2(m_run[rt], acc_l[rt][0]);
     }
+  }
   }
 }
 
-// fp32 cache: sixteen query rows of one (sequence, KV head) and a split of its
-// pages per workgroup, on the fp32 matrix instruction (attn_f32.h).
+// fp32 cache: blocks of sixteen query rows, on the fp32 matrix instruction
+// (attn_f32.h).
 template <int NC>
 __global__ __launch_bounds__(64 * kWavesF32Attn) void k_tree_attn_f32(TreeAttn a) {
-  const int i = blockIdx.z, g = blockIdx.y;
-  const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
-  const int G = a.n_q / a.kv.n_kv, rows = n * a.np * G, DH = a.kv.d_h;
-  const int blk = blockIdx.x / a.max_splits, split = blockIdx.x % a.max_splits;
-  const int npages = (len + 15) >> 4;
-  int each;
-  const int nsplit = tree_splits(npages, a.pages_per_split, &each);
-  if (blk * 16 >= rows || split >= nsplit) return;
-  const int pb = split * each, pe = min(npages, pb + each);
-  const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
   __shared__ F32Merge<NC> mg;
   __shared__ uint64_t line_s[kTreeNodes];
-  if (threadIdx.x < 64) line_s[threadIdx.x] = node_line(a.parents + first, n);
-  __syncthreads();
-  const int rho = blk * 16 + (threadIdx.x & 15);
-  const bool live = rho < rows;
-  const SeesLine sees{base, live ? line_s[rho / (G * a.np)] : 0};
-  attn_f32<NC>(mg, (const float *)a.Q + place(live ? rho : 0) * DH, live, sees, base >> 4, len, (const float *)a.kv.k,
-               (const float *)a.kv.v, a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps, pb, pe, a.kv.n_kv, g, DH);
-  for (int e = threadIdx.x; e < min(16, rows - blk * 16) * DH; e += 64 * kWavesF32Attn) {
-    const int qr = e / DH, dh = e % DH;
-    float o, l, mx;
-    mg.merged(qr, dh, o, l, mx);
-    if (nsplit == 1) {
-      ((float *)a.O)[place(blk * 16 + qr) * DH + dh] = o / l;
-    } else {
-      const size_t at = ((size_t)a.s.part[i] + (size_t)split * rows + blk * 16 + qr) * a.kv.n_kv + g;
-      a.opart[at * DH + dh] = o;
-      if (dh == 0) *(float2 *)(a.ostat + at * 2) = make_float2(mx, l);
+  const int G = a.n_q / a.kv.n_kv, DH = a.kv.d_h;
+  const int w = schedule_place(blockIdx.x, gridDim.x), end = min(a.s.first[a.s.n], (w + 1) * a.s.per);
+  for (int s = w * a.s.per; s < end;) {
+    const Piece pc = piece_at(a, s, end);
+    s += a.s.whole ? 1 : pc.st1 - pc.st0;
+    const int i = pc.i, g = pc.g;
+    const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
+    const int rows = n * a.np * G, row0 = pc.blk * 16;
+    const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
+    __syncthreads();  // (the last piece's readers)
+    if (threadIdx.x < 64) line_s[threadIdx.x] = node_line(a.parents + first, n);
+    __syncthreads();
+    const int rho = row0 + (threadIdx.x & 15);
+    const bool live = rho < rows;
+    const SeesLine sees{base, live ? line_s[rho / (G * a.np)] : 0};
+    attn_f32<NC>(mg, (const float *)a.Q + place(live ? rho : 0) * DH, live, sees, base >> 4, len, (const float *)a.kv.k,
+                 (const float *)a.kv.v, a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps, pc.st0 * kTreeStagePages,
+                 min((len + 15) >> 4, pc.st1 * kTreeStagePages), a.kv.n_kv, g, DH);
+    for (int e = threadIdx.x; e < min(16, rows - row0) * DH; e += 64 * kWavesF32Attn) {
+      const int qr = e / DH, dh = e % DH;
+      float o, l, mx;
+      mg.merged(qr, dh, o, l, mx);
+      if (pc.is_whole()) {
+        ((float *)a.O)[place(row0 + qr) * DH + dh] = o / l;
+      } else {
+        const size_t at = (size_t)pc.slot(w) * a.block + qr;
+        a.opart[at * DH + dh] = o;
+        if (dh == 0) *(float2 *)(a.ostat + at * 2) = make_float2(mx, l);
+      }
     }
   }
 }
 
-// Splits of a sequence merged in split order: one thread per (query row, four
+// The pieces of every cut unit merged in order: one thread per (query row, four
 // dimensions).
 template <typename T>
 __global__ __launch_bounds__(256) void k_tree_combine(TreeAttn a) {
   const int i = blockIdx.z, g = blockIdx.y, DH = a.kv.d_h, Q4 = DH / 4;
-  const int first = a.s.off[i], n = a.s.off[i + 1] - first;
-  const int G = a.n_q / a.kv.n_kv, rows = n * a.np * G;
-  int each;
-  const int nsplit = tree_splits((a.s.base[i] + n + 15) >> 4, a.pages_per_split, &each);
+  const int first = a.s.off[i], rows = seq_rows(a, i), stages = seq_stages(a, i), nblk = (rows + a.block - 1) / a.block;
   const int e = blockIdx.x * 256 + threadIdx.x, rho = e / Q4, d4 = e % Q4;
-  if (nsplit == 1 || rho >= rows) return;
-  const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
-  const size_t at0 = ((size_t)a.s.part[i] + rho) * a.kv.n_kv + g, step = (size_t)rows * a.kv.n_kv;
+  if (rho >= rows) return;
+  const int blk = rho / a.block, s0 = a.s.first[i] + (g * nblk + blk) * stages;
+  const int w0 = s0 / a.s.per, w1 = (s0 + stages - 1) / a.s.per;
+  if (w0 == w1) return;  // written whole
+  const RowPlace place{a.n_q / a.kv.n_kv, a.np, first, g, a.n_q, a.path_rows};
+  // workgroup w's piece begins the unit only for w0
+  auto row = [&](int w) { return (size_t)(2 * w + (w == w0)) * a.block + rho - blk * a.block; };
   float mx = kNoScore;
 #pragma unroll 8
-  for (int s = 0; s < nsplit; ++s) mx = fmaxf(mx, a.ostat[(at0 + s * step) * 2]);
+  for (int w = w0; w <= w1; ++w) mx = fmaxf(mx, a.ostat[row(w) * 2]);
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   float l = 0.f;
 #pragma unroll 8
-  for (int s = 0; s < nsplit; ++s) {
-    const size_t at = at0 + s * step;
-    const float2 ml = *(const float2 *)(a.ostat + at * 2);
+  for (int w = w0; w <= w1; ++w) {
+    const float2 ml = *(const float2 *)(a.ostat + row(w) * 2);
     const float f = exp2f(ml.x - mx);
-    const float4 v = ((const float4 *)(a.opart + at * DH))[d4];
+    const float4 v = ((const float4 *)(a.opart + row(w) * DH))[d4];
     o.x += v.x * f;
     o.y += v.y * f;
     o.z += v.z * f;
@@ -481,16 +533,16 @@ int tree_block_rows(int rows, int dtype) {
 }
 
 hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st) {
-  const int rows = a.max_nodes * a.np * (a.n_q / a.kv.n_kv), cap = tree_block_rows(rows, a.dtype);
-  if (a.s.n < 1 || a.s.n > kTreeSeqs || a.max_nodes < 1 || a.max_nodes > kTreeNodes || a.max_splits < 1 || a.pages_per_split < 1 ||
-      a.pages_per_split + kTreeStagePages > kTreeMaxPages)  // (splits are rounded up to whole stages)
+  const int rows = a.max_nodes * a.np * (a.n_q / a.kv.n_kv);
+  if (a.s.n < 1 || a.s.n > kTreeSeqs || a.max_nodes < 1 || a.max_nodes > kTreeNodes || a.s.per < 1 ||
+      a.block != tree_block_rows(rows, a.dtype) || (!a.s.whole && (!a.opart || !a.ostat)))
     return hipErrorInvalidValue;
-  const dim3 grid((rows + cap - 1) / cap * a.max_splits, a.kv.n_kv, a.s.n);
+  const dim3 grid((a.s.first[a.s.n] + a.s.per - 1) / a.s.per);
   if (a.dtype == 1) {
     if (a.kv.d_h != 128) return hipErrorInvalidValue;
     auto go = [&](auto q) {
       typedef decltype(q) QT;
-      switch (cap) {
+      switch (a.block) {
         case 16: hipLaunchKernelGGL((k_tree_attn_bf16<1, 1, 4, QT>), grid, dim3(256), 0, st, a); break;
         case 32: hipLaunchKernelGGL((k_tree_attn_bf16<2, 1, 4, QT>), grid, dim3(256), 0, st, a); break;
         case 64: hipLaunchKernelGGL((k_tree_attn_bf16<2, 2, 4, QT>), grid, dim3(512), 0, st, a); break;
@@ -515,7 +567,7 @@ hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st) {
     }
   }
   if (const hipError_t e = hipGetLastError()) return e;
-  if (a.max_splits > 1) {
+  if (!a.s.whole) {
     const dim3 cgrid((rows * (a.kv.d_h / 4) + 255) / 256, a.kv.n_kv, a.s.n);
     if (a.dtype == 1)
       hipLaunchKernelGGL(k_tree_combine<uint16_t>, cgrid, dim3(256), 0, st, a);
