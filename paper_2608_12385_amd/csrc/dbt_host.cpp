@@ -489,7 +489,7 @@ dbt_status flush(dbt_kv *kv, const int *h_pos, int npos, hipStream_t st, StepBeg
 struct TreePlan {
   std::vector<TreeSeqs> groups;
   const int *parents = nullptr;
-  int nodes = 0, max_nodes = 0, block = 0;
+  int nodes = 0, max_nodes = 0, block = 0, blocks = 0;
   float *opart = nullptr, *ostat = nullptr;
   PromptRow *map = nullptr;
 };
@@ -516,6 +516,7 @@ hipError_t tree_attn(const TreePlan &t, TreeAttn a, hipStream_t st) {
   a.parents = t.parents;
   a.max_nodes = t.max_nodes;
   a.block = t.block;
+  a.blocks = t.blocks;
   a.opart = t.opart;
   a.ostat = t.ostat;
   for (const TreeSeqs &s : t.groups) {
@@ -1368,7 +1369,7 @@ dbt_status decode_step_impl(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, int
 // unit (its stages take most of the LDS).  In pages of reading time (8 KB of keys
 // and values each): a piece's start, the merge's launch, and kTreeMergeRows rows' partial
 // results written and read (512 bytes each way).
-constexpr int kTreeStart = 6, kTreeMerge = 14, kTreeMergeRows = 8;
+constexpr int kTreeStart = 6, kTreeMerge = 14, kTreeMergeRows = 8, kTreePieces = 16;
 
 // may_be_empty: calls without a launch over the nodes
 dbt_status check_tree(const dbt_kv *kv, const dbt_tree *t, int *nodes, bool may_be_empty = false) {
@@ -1429,9 +1430,14 @@ struct TreeLayout {
 };
 TreeLayout tree_layout(const dbt_config &c, int nodes) {
   TreeLayout L;
-  // cut units leave two pieces a workgroup at most
+  // cut units leave two pieces a run at most; the runs' blocks together are no
+  // more than a round of workgroups, or one run's
   const int rows = std::min(nodes, DBT_TREE_NODES) * (1 + n_branches(c)) * (c.n_q_heads / c.n_kv_heads);
-  const size_t slots = (size_t)2 * kComputeUnits * tree_block_rows(rows, c.dtype);
+  size_t slots = 0;  // in rows
+  for (int r = 1; r <= rows; ++r) {
+    const int block = tree_block_rows(r, c.dtype), blocks = (r + block - 1) / block;
+    slots = std::max(slots, (size_t)2 * std::max(1, tree_workgroups(block, c.dtype) / blocks) * blocks * block);
+  }
   L.map = 0;
   L.opart = align256((size_t)nodes * sizeof(PromptRow));
   L.ostat = L.opart + align256(slots * c.head_dim * 4);
@@ -1440,31 +1446,28 @@ TreeLayout tree_layout(const dbt_config &c, int nodes) {
 }
 
 // The schedule of up to kTreeSeqs sequences (see TreeSeqs): whole units, or equal
-// runs for kComputeUnits workgroups, whichever the estimate above makes shorter.
-void schedule_tree(const dbt_config &c, int n_paths, int block, TreeSeqs *g) {
-  const int G = c.n_q_heads / c.n_kv_heads;
-  long long units = 0, total = 0;
+// runs for one round of workgroups, whichever the estimate above makes shorter.
+void schedule_tree(const dbt_config &c, int block, int blocks, TreeSeqs *g) {
+  long long total = 0;
   int longest = 0;
   auto stages = [&](int i) {
     const int pages = (g->base[i] + g->off[i + 1] - g->off[i] + kPage - 1) / kPage;
     return (pages + kTreeStagePages - 1) / kTreeStagePages;
   };
-  auto of_seq = [&](int i) {
-    return (long long)c.n_kv_heads * (((g->off[i + 1] - g->off[i]) * n_paths * G + block - 1) / block);
-  };
   for (int i = 0; i < g->n; ++i) {
-    units += of_seq(i);
-    total += of_seq(i) * stages(i);
+    total += (long long)c.n_kv_heads * stages(i);
     longest = std::max(longest, stages(i));
   }
-  const long long rounds = (units + kComputeUnits - 1) / kComputeUnits, run = (total + kComputeUnits - 1) / kComputeUnits;
-  const long long P = kTreeStagePages;
-  const long long whole = (units <= kComputeUnits ? longest * P : std::max(longest * P, run * P + longest * P / 2)) + rounds * kTreeStart;
-  const long long cut = run * P + 2 * (kTreeStart + block / kTreeMergeRows) + kTreeMerge;
+  const long long units = (long long)g->n * c.n_kv_heads, W = std::max(1, tree_workgroups(block, c.dtype) / blocks);
+  // (a unit in at most kTreePieces pieces: the merge reads eight at a time)
+  const long long rounds = (units + W - 1) / W, P = kTreeStagePages,
+                  run = std::max<long long>((total + W - 1) / W, (longest + kTreePieces - 1) / kTreePieces);
+  const long long whole = (units <= W ? longest * P : std::max(longest * P, run * P + longest * P / 2)) + rounds * kTreeStart;
+  const long long cut = run * P + 2 * kTreeStart + block / kTreeMergeRows + kTreeMerge;
   g->whole = whole <= cut;
   g->per = g->whole ? 1 : (int)run;
   g->first[0] = 0;
-  for (int i = 0; i < g->n; ++i) g->first[i + 1] = g->first[i] + (int)of_seq(i) * (g->whole ? 1 : stages(i));
+  for (int i = 0; i < g->n; ++i) g->first[i + 1] = g->first[i] + c.n_kv_heads * (g->whole ? 1 : stages(i));
 }
 
 // base[b]: positions of sequence b before its nodes.
@@ -1478,7 +1481,9 @@ TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths
   p.opart = (float *)(ws + L.opart);
   p.ostat = (float *)(ws + L.ostat);
   for (int b = 0; b < t->batch; ++b) p.max_nodes = std::max(p.max_nodes, t->h_nodes[b]);
-  p.block = tree_block_rows(p.max_nodes * n_paths * (cf.n_q_heads / cf.n_kv_heads), cf.dtype);
+  const int rows = p.max_nodes * n_paths * (cf.n_q_heads / cf.n_kv_heads);
+  p.block = tree_block_rows(rows, cf.dtype);
+  p.blocks = (rows + p.block - 1) / p.block;
   int off = 0;
   for (int b = 0; b < t->batch; ++b) {
     const int n = t->h_nodes[b];
@@ -1494,7 +1499,7 @@ TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths
     off += n;
     g.off[++g.n] = off;
   }
-  for (TreeSeqs &g : p.groups) schedule_tree(cf, n_paths, p.block, &g);
+  for (TreeSeqs &g : p.groups) schedule_tree(cf, p.block, p.blocks, &g);
   return p;
 }
 

@@ -356,12 +356,12 @@ hipError_t launch_attn_prefill(const PromptAttn &a, hipStream_t st);
 // Sequences of a tree call that have nodes: sequence seq[i] has base[i]
 // positions before its nodes, which are rows off[i] .. off[i + 1] - 1 of the call.
 //
-// The attention's work is units of one (sequence, KV head, block of query
-// rows), sequence by sequence, blocks next to each other; a unit is its pages in
-// stages of kTreeStagePages.  Either every workgroup takes a whole unit
-// (whole), or all of them equal runs of `per` stages of the units in a row, so
-// that units are cut where runs end; first[i] counts the units (whole) or
-// stages before those of sequence i.
+// The attention's work is units of one (sequence, KV head), sequence by
+// sequence; a unit is its pages in stages of kTreeStagePages.  Either every
+// workgroup takes a whole unit (whole), or all of them equal runs of `per`
+// stages of the units in a row, so that units are cut where runs end; first[i]
+// counts the units (whole) or stages before those of sequence i.  Query rows
+// beyond one workgroup's go to further workgroups with the same run.
 constexpr int kTreeSeqs = 128;
 constexpr int kTreeNodes = 64;  // DBT_TREE_NODES: one lane, one bit of a line of ancestors each
 constexpr int kTreeStagePages = 8;
@@ -382,14 +382,16 @@ struct TreeAttn {
   int n_q, np;        // query heads, paths
   int dtype;
   int max_nodes;      // of one sequence of the call
-  int block;          // tree_block_rows of it
-  float *opart;       // [2 * workgroups][block][d_h]: the pieces of units cut by runs
-  float *ostat;       // [2 * workgroups][block][2]
+  int block, blocks;  // tree_block_rows of it, and the blocks of its rows
+  float *opart;       // [2 * runs][blocks][block][d_h]: the pieces of units cut by runs
+  float *ostat;       // [2 * runs][blocks][block][2]
 };
 hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st);
-// Query rows of one unit, at most, where a sequence has up to `rows` for a KV head
+// Query rows of one workgroup where a sequence has up to `rows` for a KV head
 // (nodes x paths x query heads of the KV head).
 int tree_block_rows(int rows, int dtype);
+// Workgroups of the kernel for such blocks that run at a time.
+int tree_workgroups(int block, int dtype);
 // Kept nodes of up to kKeepSeqs sequences: node path[i][j] of sequence seq[i]
 // moves to position base[i] + j, j = first[i] .. count[i] - 1 (those before
 // stay where they are).

@@ -47,14 +47,13 @@ struct RowPlace {
   }
 };
 
-// The next piece of work of workgroup w at position s of the schedule
-// (TreeSeqs): stages st0 .. st1 - 1 of unit (sequence i, KV head g, block blk),
-// which has `stages` of them.
+// The next piece of work of run w at position s of the schedule (TreeSeqs):
+// stages st0 .. st1 - 1 of unit (sequence i, KV head g), which has `stages`.
 struct Piece {
-  int i, g, blk, st0, st1, stages;
+  int i, g, st0, st1, stages;
   __device__ __forceinline__ bool is_whole() const { return st0 == 0 && st1 == stages; }
-  // A workgroup has at most one piece that begins inside a unit (its first)
-  // and one that begins a unit without ending it (its last).
+  // A run has at most one piece that begins inside a unit (its first) and one
+  // that begins a unit without ending it (its last).
   __device__ __forceinline__ int slot(int w) const { return 2 * w + (st0 == 0); }
 };
 __device__ __forceinline__ int seq_rows(const TreeAttn &a, int i) {
@@ -65,26 +64,26 @@ __device__ __forceinline__ int seq_stages(const TreeAttn &a, int i) {
   return (pages + kTreeStagePages - 1) / kTreeStagePages;
 }
 __device__ __forceinline__ Piece piece_at(const TreeAttn &a, int s, int end) {
-  int lo = 0, hi = a.s.n;  // first[lo] <= s < first[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (a.s.first[mid] <= s) lo = mid;
-    else hi = mid;
-  }
+  // the sequence: as many of first[0 .. n) are at most s, counted by the wave
+  // (a search would wait for one argument after the other)
+  const int lane = threadIdx.x & 63;
+  int lo = -1;
+#pragma unroll
+  for (int k = 0; k < kTreeSeqs; k += 64) lo += __popcll(__ballot(k + lane < a.s.n && a.s.first[k + lane] <= s));
   Piece p;
   p.i = lo;
   p.stages = seq_stages(a, lo);
   const int len = a.s.whole ? 1 : p.stages, rem = s - a.s.first[lo], unit = rem / len;
-  const int nblk = (seq_rows(a, lo) + a.block - 1) / a.block;
-  p.blk = unit % nblk;
-  p.g = unit / nblk;
+  p.g = unit;
   p.st0 = a.s.whole ? 0 : rem % len;
   p.st1 = a.s.whole ? p.stages : min(p.stages, p.st0 + end - s);
   return p;
 }
 // Workgroups are dealt to the eight XCDs in turn: workgroup b takes a place that
-// keeps neighbours of the schedule (blocks of one (sequence, KV head), which
-// read the same pages) on one XCD and its L2.
+// keeps neighbours on one XCD.  Those are the blocks of one run, which read the
+// same pages at the same time: all but the first of them from the XCD's L2
+// (8 x 16k-32k positions, two blocks: 0.8 GB from memory; with each block's runs cut
+// where they come, so that the two meet at other times, 1.6 GB).
 __device__ __forceinline__ int schedule_place(int b, int n) {
   const int x = b & 7, q = n >> 3, r = n & 7;
   return x * q + min(x, r) + (b >> 3);
@@ -111,14 +110,14 @@ constexpr float kLazyMargin = 8.f;
 //
 // Bound: 16 rows and up to 128 per key read at the memory's rate; 256 rows by
 // the vector unit's softmax beside the matrix unit.
-template <int RT, int RW, int KW, typename QT>
-__global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(RW *KW / 4, RW *KW / 4))) void
+template <int RT, int RW, int KW, int SP, typename QT>
+__global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(RW *KW * (SP == 4 ? 2 : 1) / 4, RW *KW * (SP == 4 ? 2 : 1) / 4))) void
 k_tree_attn_bf16(TreeAttn a) {
-  constexpr int DH = 128, NW = RW * KW, PP = 4 / KW, PB = 16 * DH;  // PP: pairs of a stage per wave; PB: elements of a page
-  static_assert(kTreeStagePages == 8 && KW * PP == 4, "four pairs per stage");
+  constexpr int DH = 128, NW = RW * KW, PP = SP / 2 / KW, PB = 16 * DH;  // PP: pairs of a stage per wave; PB: elements of a page
+  static_assert(kTreeStagePages % SP == 0 && KW * PP * 2 == SP && SP % NW == 0, "whole pairs and pages for every wave");
   // two sets of stage buffers, separate arrays so that the loads filling one
   // set are told apart from the reads of the other
-  __shared__ __attribute__((aligned(16))) uint16_t kl0[8 * PB], vl0[8 * PB], kl1[8 * PB], vl1[8 * PB];
+  __shared__ __attribute__((aligned(16))) uint16_t kl0[SP * PB], vl0[SP * PB], kl1[SP * PB], vl1[SP * PB];
   __shared__ int pid_s[kWindow * kTreeStagePages];
   __shared__ uint64_t line_s[kTreeNodes];
   __shared__ float ms[KW][RW * RT][16], ls[KW][RW * RT][16];
@@ -127,19 +126,51 @@ k_tree_attn_bf16(TreeAttn a) {
   const int r = lane & 15, gq = lane >> 4;
   const int n_kv = a.kv.n_kv, G = a.n_q / n_kv;
   const float scale = kLog2e / sqrtf((float)DH);
-  const int w = schedule_place(blockIdx.x, gridDim.x), end = min(a.s.first[a.s.n], (w + 1) * a.s.per);
+  const int place_w = schedule_place(blockIdx.x, gridDim.x), w = place_w / a.blocks, blk = place_w % a.blocks;
+  const int end = min(a.s.first[a.s.n], (w + 1) * a.s.per);
   for (int at = w * a.s.per; at < end;) {
   const Piece pc = piece_at(a, at, end);
   at += a.s.whole ? 1 : pc.st1 - pc.st0;
   const int i = pc.i, g = pc.g;
   const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
-  const int rows = n * a.np * G, row0 = pc.blk * (RW * RT * 16);
+  const int rows = n * a.np * G, row0 = blk * (RW * RT * 16);
+  if (row0 >= rows) continue;
   const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
   const int *ptab = a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps;
   const int pages0 = pc.st0 * 8, pages1 = min((len + 15) >> 4, pc.st1 * 8);  // the piece's pages
+  int pb = pages0, npg = min(pages1 - pb, kWindow * 8);  // the window's first page, its pages
   __syncthreads();  // (the last piece's readers)
+  for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
   if (wave == 0) line_s[lane] = node_line(a.parents + first, n);
   __syncthreads();
+
+  // K row j of a page holds its 16-byte chunk c at c ^ kswz(j): the score operand
+  // reads rows {0..3, 8..11} (or {4..7, 12..15}) of both pages at one chunk
+  // without bank conflicts.  V rows (one dimension, 32 bytes) need no swizzle.
+  auto kswz = [](int row) { return ((row & 3) | ((row >> 3) << 2)) << 1; };
+  const uint16_t *kbase = (const uint16_t *)a.kv.k, *vbase = (const uint16_t *)a.kv.v;
+  // A stage is 64 loads of 1 KB, four of K and four of V a page: each wave takes
+  // 64 / NW.  Pages past the split's last re-read it (never used unmasked).
+  auto dma = [&](int st, uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < SP / NW; ++p) {
+      const int page = wave * (SP / NW) + p;
+      const int phys = __builtin_amdgcn_readfirstlane(pid_s[min(st * SP + page, npg - 1)]);
+      const size_t at = ((size_t)phys * n_kv + g) * PB;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int row = 4 * j + (lane >> 4);
+        __builtin_amdgcn_global_load_lds((const void *)(kbase + at + row * DH + ((lane & 15) ^ kswz(row)) * 8),
+                                         (lds_void *)(kb + page * PB + 4 * j * DH), 16, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        __builtin_amdgcn_global_load_lds((const void *)(vbase + at + 32 * j * 16 + lane * 8),
+                                         (lds_void *)(vb + page * PB + 32 * j * 16), 16, 0, 0);
+    }
+  };
+
+  dma(0, kl0, vl0);  // (the queries' loads run beside it)
 
   const int wrow = row0 + rw * RT * 16;  // the wave's first row
   u32x4 qf[RT][4];
@@ -161,33 +192,6 @@ k_tree_attn_bf16(TreeAttn a) {
       if (!live) qf[rt][s] = u32x4{0, 0, 0, 0};
     }
   }
-
-  // K row j of a page holds its 16-byte chunk c at c ^ kswz(j): the score operand
-  // reads rows {0..3, 8..11} (or {4..7, 12..15}) of both pages at one chunk
-  // without bank conflicts.  V rows (one dimension, 32 bytes) need no swizzle.
-  auto kswz = [](int row) { return ((row & 3) | ((row >> 3) << 2)) << 1; };
-  const uint16_t *kbase = (const uint16_t *)a.kv.k, *vbase = (const uint16_t *)a.kv.v;
-  int pb = 0, npg = 0;  // the window's first page, its pages
-  // A stage is 64 loads of 1 KB, four of K and four of V a page: each wave takes
-  // 64 / NW.  Pages past the split's last re-read it (never used unmasked).
-  auto dma = [&](int st, uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
-#pragma unroll
-    for (int p = 0; p < 8 / NW; ++p) {
-      const int page = wave * (8 / NW) + p;
-      const int phys = __builtin_amdgcn_readfirstlane(pid_s[min(st * 8 + page, npg - 1)]);
-      const size_t at = ((size_t)phys * n_kv + g) * PB;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int row = 4 * j + (lane >> 4);
-        __builtin_amdgcn_global_load_lds((const void *)(kbase + at + row * DH + ((lane & 15) ^ kswz(row)) * 8),
-                                         (lds_void *)(kb + page * PB + 4 * j * DH), 16, 0, 0);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        __builtin_amdgcn_global_load_lds((const void *)(vbase + at + 32 * j * 16 + lane * 8),
-                                         (lds_void *)(vb + page * PB + 32 * j * 16), 16, 0, 0);
-    }
-  };
 
   float m_run[RT];
   floatx4 acc[RT][8], acc_l[RT];  // acc_l: the sums of the rounded probabilities, by one more value multiply with V = 1
@@ -245,58 +249,71 @@ k_tree_attn_bf16(TreeAttn a) {
         }
       }
     }
+    // (the row tiles' steps side by side: one tile alone leaves the units waiting
+    // for its chain of maximum, exponentials and conversion)
+    float s[RT][8], m_new[RT];
+    bool grow = false;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      float s[8];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        s[e] = sc[rt][0][e];
-        s[4 + e] = sc[rt][1][e];
+        s[rt][e] = sc[rt][0][e];
+        s[rt][4 + e] = sc[rt][1][e];
       }
-      uint32_t seen = 0xff;
       if (MASKED) {  // the row's eight positions: before `base`, or on its line
         const int rel = kp0 - base;
-        seen = !page_ok || rel >= 64 ? 0u
-               : rel >= 0            ? (uint32_t)(line[rt] >> rel) & 0xff
-               : rel > -8            ? (uint32_t)((line[rt] << -rel) | ((1u << -rel) - 1)) & 0xff
-                                     : 0xffu;
+        const uint32_t seen = !page_ok || rel >= 64 ? 0u
+                              : rel >= 0            ? (uint32_t)(line[rt] >> rel) & 0xff
+                              : rel > -8            ? (uint32_t)((line[rt] << -rel) | ((1u << -rel) - 1)) & 0xff
+                                                    : 0xffu;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (!((seen >> e) & 1)) s[e] = -INFINITY;
+          if (!((seen >> e) & 1)) s[rt][e] = -INFINITY;
       }
-      float mt = s[0];
+      float mt = s[rt][0];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) mt = fmaxf(mt, s[e]);
+      for (int e = 1; e < 8; ++e) mt = fmaxf(mt, s[rt][e]);
       // lazy rescaling: a row's base moves only when the pair's maximum exceeds it
       // by more than kLazyMargin, so exponentials stay <= 2^kLazyMargin
       const float mt_s = rows4_max(mt) * scale;
-      const bool grow = mt_s > m_run[rt] + kLazyMargin;
-      const float m_new = grow ? mt_s : m_run[rt];
-      float p[8];
+      const bool up = mt_s > m_run[rt] + kLazyMargin;
+      m_new[rt] = up ? mt_s : m_run[rt];
+      grow |= up;
+    }
+    if (__any(grow)) {  // (a factor of exactly 1 where the base stays)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[e], scale, -m_new));
-      if (__any(grow)) {
-        const float corr = __builtin_amdgcn_exp2f(m_run[rt] - m_new);
+      for (int rt = 0; rt < RT; ++rt) {
+        const float corr = __builtin_amdgcn_exp2f(m_run[rt] - m_new[rt]);
         acc_l[rt] = acc_l[rt] * corr;
 #pragma unroll
         for (int c = 0; c < 8; ++c) acc[rt][c] = acc[rt][c] * corr;
+        m_run[rt] = m_new[rt];
       }
-      m_run[rt] = m_new;
+    }
+    u32x4 pf[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][e], scale, -m_new[rt]));
       // (probabilities are rounded to bf16 for the matrix unit; their sum is of the rounded ones)
-      const u32x4 pf = u32x4{pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7])};
+      pf[rt] = u32x4{pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7])};
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
       acc_l[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones),
-                                                          __builtin_bit_cast(bf16x8, pf), acc_l[rt], 0, 0, 0);
+                                                          __builtin_bit_cast(bf16x8, pf[rt]), acc_l[rt], 0, 0, 0);
 #pragma unroll
       for (int c = 0; c < 8; ++c)
         acc[rt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[c]),
-                                                             __builtin_bit_cast(bf16x8, pf), acc[rt][c], 0, 0, 0);
+                                                             __builtin_bit_cast(bf16x8, pf[rt]), acc[rt][c], 0, 0, 0);
     }
   };
   auto stage = [&](int st, const uint16_t *kb, const uint16_t *vb, auto masked) __attribute__((always_inline)) {
     if (!active) return;
 #pragma unroll 1
     for (int j = 0; j < PP; ++j) {
-      const int pi = kw * PP + j, pg0 = st * 8 + 2 * pi;
+      const int pi = kw * PP + j, pg0 = st * SP + 2 * pi;
       if (decltype(masked)::value && pg0 >= npg) break;
       pair(pg0, kb + 2 * pi * PB, vb + 2 * pi * PB, masked);
     }
@@ -305,13 +322,8 @@ k_tree_attn_bf16(TreeAttn a) {
   // the other set, which the next stage's loads then fill.  Stages of which
   // every row sees every key first, in pairs so that each set is known; then
   // the last ones, those from the page of position `base` on.
-  for (pb = pages0; pb < pages1; pb += kWindow * 8) {
-    npg = min(pages1 - pb, kWindow * 8);
-    __syncthreads();
-    for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
-    __syncthreads();
-    const int nst = (npg + 7) >> 3, nfull = max(0, min(npg, (base >> 4) - pb)) >> 3;
-    dma(0, kl0, vl0);
+  for (;;) {
+    const int nst = (npg + SP - 1) / SP, nfull = max(0, min(npg, (base >> 4) - pb)) / SP;
     for (int st = 0; st < nfull; st += 2) {
       __syncthreads();
       if (st + 1 < nst) dma(st + 1, kl1, vl1);
@@ -331,6 +343,13 @@ k_tree_attn_bf16(TreeAttn a) {
       if (st + 1 < nst) dma(st + 1, set1 ? kl0 : kl1, set1 ? vl0 : vl1);
       stage(st, set1 ? kl1 : kl0, set1 ? vl1 : vl0, std::true_type{});
     }
+    pb += kWindow * 8;
+    if (pb >= pages1) break;
+    npg = min(pages1 - pb, kWindow * 8);
+    __syncthreads();
+    for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
+    __syncthreads();
+    dma(0, kl0, vl0);
   }
 
   if (__any(odd)) {
@@ -410,7 +429,7 @@ k_tree_attn_bf16(TreeAttn a) {
       for (int c = 0; c < 8; ++c)
         *(u32x2 *)(o + 16 * c) = u32x2{pack2(acc[rt][c][0] * inv, acc[rt][c][1] * inv), pack2(acc[rt][c][2] * inv, acc[rt][c][3] * inv)};
     } else {
-      const size_t to = (size_t)pc.slot(w) * a.block + rho - row0;
+      const size_t to = ((size_t)pc.slot(w) * a.blocks + blk) * a.block + rho - row0;
 #pragma unroll
       for (int c = 0; c < 8; ++c)
         *(float4 *)(a.opart + to * DH + 16 * c + 4 * gq) = make_float4(acc[rt][c][0], acc[rt][c][1], acc[rt][c][2], acc[rt][c][3]);
@@ -427,13 +446,15 @@ __global__ __launch_bounds__(64 * kWavesF32Attn) void k_tree_attn_f32(TreeAttn a
   __shared__ F32Merge<NC> mg;
   __shared__ uint64_t line_s[kTreeNodes];
   const int G = a.n_q / a.kv.n_kv, DH = a.kv.d_h;
-  const int w = schedule_place(blockIdx.x, gridDim.x), end = min(a.s.first[a.s.n], (w + 1) * a.s.per);
+  const int place_w = schedule_place(blockIdx.x, gridDim.x), w = place_w / a.blocks, blk = place_w % a.blocks;
+  const int end = min(a.s.first[a.s.n], (w + 1) * a.s.per);
   for (int s = w * a.s.per; s < end;) {
     const Piece pc = piece_at(a, s, end);
     s += a.s.whole ? 1 : pc.st1 - pc.st0;
     const int i = pc.i, g = pc.g;
     const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
-    const int rows = n * a.np * G, row0 = pc.blk * 16;
+    const int rows = n * a.np * G, row0 = blk * 16;
+    if (row0 >= rows) continue;
     const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
     __syncthreads();  // (the last piece's readers)
     if (threadIdx.x < 64) line_s[threadIdx.x] = node_line(a.parents + first, n);
@@ -451,7 +472,7 @@ __global__ __launch_bounds__(64 * kWavesF32Attn) void k_tree_attn_f32(TreeAttn a
       if (pc.is_whole()) {
         ((float *)a.O)[place(row0 + qr) * DH + dh] = o / l;
       } else {
-        const size_t at = (size_t)pc.slot(w) * a.block + qr;
+        const size_t at = ((size_t)pc.slot(w) * a.blocks + blk) * 16 + qr;
         a.opart[at * DH + dh] = o;
         if (dh == 0) *(float2 *)(a.ostat + at * 2) = make_float2(mx, l);
       }
@@ -464,30 +485,44 @@ __global__ __launch_bounds__(64 * kWavesF32Attn) void k_tree_attn_f32(TreeAttn a
 template <typename T>
 __global__ __launch_bounds__(256) void k_tree_combine(TreeAttn a) {
   const int i = blockIdx.z, g = blockIdx.y, DH = a.kv.d_h, Q4 = DH / 4;
-  const int first = a.s.off[i], rows = seq_rows(a, i), stages = seq_stages(a, i), nblk = (rows + a.block - 1) / a.block;
+  const int first = a.s.off[i], rows = seq_rows(a, i), stages = seq_stages(a, i);
   const int e = blockIdx.x * 256 + threadIdx.x, rho = e / Q4, d4 = e % Q4;
   if (rho >= rows) return;
-  const int blk = rho / a.block, s0 = a.s.first[i] + (g * nblk + blk) * stages;
+  const int s0 = a.s.first[i] + g * stages;
   const int w0 = s0 / a.s.per, w1 = (s0 + stages - 1) / a.s.per;
   if (w0 == w1) return;  // written whole
   const RowPlace place{a.n_q / a.kv.n_kv, a.np, first, g, a.n_q, a.path_rows};
-  // workgroup w's piece begins the unit only for w0
-  auto row = [&](int w) { return (size_t)(2 * w + (w == w0)) * a.block + rho - blk * a.block; };
-  float mx = kNoScore;
-#pragma unroll 8
-  for (int w = w0; w <= w1; ++w) mx = fmaxf(mx, a.ostat[row(w) * 2]);
+  // run w's piece begins the unit only for w0
+  auto row = [&](int w) { return (size_t)(2 * w + (w == w0)) * a.blocks * a.block + rho; };
+  // eight pieces at a time, all of their loads in flight together
+  float mx = kNoScore, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  float l = 0.f;
-#pragma unroll 8
-  for (int w = w0; w <= w1; ++w) {
-    const float2 ml = *(const float2 *)(a.ostat + row(w) * 2);
-    const float f = exp2f(ml.x - mx);
-    const float4 v = ((const float4 *)(a.opart + row(w) * DH))[d4];
-    o.x += v.x * f;
-    o.y += v.y * f;
-    o.z += v.z * f;
-    o.w += v.w * f;
-    l += ml.y * f;
+  for (int w = w0; w <= w1; w += 8) {
+    float2 ml[8];
+    float4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const size_t at = row(min(w + k, w1));
+      ml[k] = *(const float2 *)(a.ostat + at * 2);
+      v[k] = ((const float4 *)(a.opart + at * DH))[d4];
+    }
+    float mn = mx;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mn = fmaxf(mn, ml[k].x);
+    const float f0 = exp2f(mx - mn);
+    o = make_float4(o.x * f0, o.y * f0, o.z * f0, o.w * f0);
+    l *= f0;
+    mx = mn;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (w + k > w1) break;
+      const float f = exp2f(ml[k].x - mx);
+      o.x += v[k].x * f;
+      o.y += v[k].y * f;
+      o.z += v[k].z * f;
+      o.w += v[k].w * f;
+      l += ml[k].y * f;
+    }
   }
   T *out = (T *)a.O + place(rho) * DH + d4 * 4;
   st<T>(out, 0, o.x / l);
@@ -525,29 +560,30 @@ hipError_t launch_tree_rows(const TreeSeqs &s, const int *parents, PromptRow *ro
   return hipGetLastError();
 }
 
+int tree_workgroups(int block, int dtype) { return dtype == 1 && block < 128 ? kComputeUnits : 2 * kComputeUnits; }
+
 int tree_block_rows(int rows, int dtype) {
   if (dtype != 1) return 16;
-  for (int r = 16; r < 256; r *= 2)
+  for (int r = 16; r < 128; r *= 2)
     if (rows <= r) return r;
-  return 256;
+  return 128;
 }
 
 hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st) {
   const int rows = a.max_nodes * a.np * (a.n_q / a.kv.n_kv);
   if (a.s.n < 1 || a.s.n > kTreeSeqs || a.max_nodes < 1 || a.max_nodes > kTreeNodes || a.s.per < 1 ||
-      a.block != tree_block_rows(rows, a.dtype) || (!a.s.whole && (!a.opart || !a.ostat)))
+      a.block != tree_block_rows(rows, a.dtype) || a.blocks != (rows + a.block - 1) / a.block || (!a.s.whole && (!a.opart || !a.ostat)))
     return hipErrorInvalidValue;
-  const dim3 grid((a.s.first[a.s.n] + a.s.per - 1) / a.s.per);
+  const dim3 grid((a.s.first[a.s.n] + a.s.per - 1) / a.s.per * a.blocks);
   if (a.dtype == 1) {
     if (a.kv.d_h != 128) return hipErrorInvalidValue;
     auto go = [&](auto q) {
       typedef decltype(q) QT;
       switch (a.block) {
-        case 16: hipLaunchKernelGGL((k_tree_attn_bf16<1, 1, 4, QT>), grid, dim3(256), 0, st, a); break;
-        case 32: hipLaunchKernelGGL((k_tree_attn_bf16<2, 1, 4, QT>), grid, dim3(256), 0, st, a); break;
-        case 64: hipLaunchKernelGGL((k_tree_attn_bf16<2, 2, 4, QT>), grid, dim3(512), 0, st, a); break;
-        case 128: hipLaunchKernelGGL((k_tree_attn_bf16<2, 4, 2, QT>), grid, dim3(512), 0, st, a); break;
-        default: hipLaunchKernelGGL((k_tree_attn_bf16<2, 8, 1, QT>), grid, dim3(512), 0, st, a); break;
+        case 16: hipLaunchKernelGGL((k_tree_attn_bf16<1, 1, 4, 8, QT>), grid, dim3(256), 0, st, a); break;
+        case 32: hipLaunchKernelGGL((k_tree_attn_bf16<2, 1, 4, 8, QT>), grid, dim3(256), 0, st, a); break;
+        case 64: hipLaunchKernelGGL((k_tree_attn_bf16<2, 2, 4, 8, QT>), grid, dim3(512), 0, st, a); break;
+        default: hipLaunchKernelGGL((k_tree_attn_bf16<2, 4, 1, 4, QT>), grid, dim3(256), 0, st, a); break;
       }
     };
     if (a.q32) go(float{});
