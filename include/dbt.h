@@ -371,7 +371,8 @@ size_t dbt_sample_workspace_bytes(int32_t rows, int32_t vocab);
  * ones by index, the first top_k tokens stay, of them the shortest run whose sum
  * reaches top_p of theirs, of that those with w_v >= min_p; the row's token is the
  * lowest index at which the running sum of the weights that stayed exceeds u
- * times their sum.  prob (may be NULL) [rows]: its share of that sum.  Weights are
+ * times their sum.  prob (may be NULL) [rows]: its share of that sum (1 for
+ * a greedy token).  Weights are
  * evaluated in float64 and held as multiples of 2^-42 or a finer step, so that
  * every sum is exact and a row's token depends on nothing but its row.  A row that holds a NaN or +infinity, nothing
  * above -infinity, or an alpha outside [0, 1] gets token -1 and probability 0; u below

@@ -10,16 +10,21 @@
 //
 // top-k, top-p and min-p all keep a run from the front of the order by falling
 // weight (equal weights by index), so what stays is everything above one cut.
-// The cut is found without sorting: a histogram over 254 classes of
-// W (eight per octave) by count and mass gives the class in which it falls;
-// the tokens up to that class are listed in index order; a workgroup per row
-// ranks the class's own tokens exactly.  The draw is a prefix search over the list
-// (rows without a cut: over tile sums, then inside one tile).
+// The cut is found without sorting.  Every part of a row leaves a histogram of
+// its mass (and number) by 254 classes of W, eight an octave; the classes in which
+// the cuts can fall are known from it, and only their tokens are listed; one
+// workgroup per row places the cut among them exactly.  The histograms give
+// each part's mass above the cut, so the draw finds its part from those and reads
+// that part alone again.
 #include <cmath>
 
 #include "../../include/dbt.h"
 #include "common.h"
 #include "host_internal.h"
+
+// A token's weight is evaluated by three kernels, which have to agree on its
+// bits: fused operations are the ones written here, no others.
+#pragma clang fp contract(off)
 
 namespace {
 
@@ -28,11 +33,13 @@ typedef unsigned long long u64;
 
 constexpr int kTile = 2048;         // tokens of one statistics tile
 constexpr int kMaxVocab = 1 << 20;
-constexpr int kRowsPerCall = 128;   // rows of one launch of the first kernel (parameters travel as arguments)
+constexpr int kRowsPerCall = 224;   // rows whose parameters travel with one launch
 constexpr int kClasses = 256;       // weight classes: 0..253 by octave eighths, 254 everything lower, 255 weight zero
 constexpr int kLow = 254, kNone = 255;
-constexpr int kRankCap = 2048;      // tokens of the cut's class that are ranked in LDS
-constexpr int kFinal = 512;         // threads of the row kernel
+constexpr int kMaxScale = 46;       // s at most: the largest mixture value, within some 2^-52 of max m, has weight 2^s
+constexpr int kRankCap = 256;       // tokens that are ranked against each other
+constexpr int kFinal = 512;         // threads of the row kernels
+constexpr int kMaxParts = kMaxVocab / kTile;
 
 struct RowParams {
   float t, top_p, min_p;
@@ -43,34 +50,36 @@ struct ParamBlock {
 };
 
 struct RowState {
-  double scale[4];  // m = sum_j scale[j] exp(z_j - zmax[j])
-  double inv_t, mmax;
+  double scale[4];  // m / max m = sum_j scale[j] exp(z_j - zmax[j])
+  double inv_t;
   u64 least;        // weights below stay out (min-p; 1: nothing but zeros)
+  u64 k_mass;       // mass of the classes before kc
   float zmax[4];
   float top_p;
   float u;
   int top_k;
-  int valid, greedy, cut;  // cut: top-k or top-p remove something
-  int last;         // class of the cut: tokens of classes 0..last are listed
-  int listed;
+  int valid, greedy, cut;  // cut: top-k or top-p can remove something
+  int kc, k_need;   // class in which top-k cuts and how many of it stay (kc = -1: nothing is cut)
+  int k_whole;      // that class stays whole
+  int pl, ph;       // classes in which top-p can cut (pl > ph: none)
+  int lc;           // class of `least` (-1: no such cut)
+  unsigned listed;
 };
 
 struct Work {
   RowState *state;   // [rows]
   double2 *stats;    // [rows][tiles][4]: max, sum exp(z - max) of path j
   u64 *tmass;        // [rows][parts][256]: mass by class (rows without a cut: [0] the kept mass)
-  unsigned *tcount;  // [rows][parts][256]
-  u64 *mass;         // [rows][256]
-  unsigned *count;   // [rows][256]
-  unsigned *toff;    // [rows][parts]: place in the list of a part's first listed token
-  uint8_t *cls;      // [rows][vocab]
+  unsigned *tcount;  // [rows][parts][256] (rows with top-k)
+  u64 *upto;         // [rows][256]: mass of classes 0..c
+  uint8_t *cls;      // [rows][vocab up to 16]
   u64 *lw;           // [rows][vocab] listed weights
   int *li;           // [rows][vocab] listed tokens
 };
 
 struct Args {
   const float *z1, *z2, *alpha, *u;
-  int rows, V, nb, s;
+  int rows, V, Vp, s;
   int tiles;         // statistics tiles per row
   int parts, part;   // workgroups per row of the weighing kernels, tokens of each
   int *token;
@@ -78,36 +87,78 @@ struct Args {
   Work w;
 };
 
-template <int NP> __device__ __forceinline__ const float *path_row(const Args &a, int j, int row) {
+__device__ __forceinline__ const float *path_row(const Args &a, int j, int row) {
   return j == 0 ? a.z1 + (size_t)row * a.V : a.z2 + ((size_t)(j - 1) * a.rows + row) * a.V;
 }
 
-// Mixture value of one token: the same operations wherever it is evaluated, so
-// that the largest one divides to exactly 1.
+constexpr double kLog2eD = 1.4426950408889634074;
+
+// 2^t for t <= 0 (and small t above), within 1e-14: t = n + f, |f| <= 1/2, and the
+// Taylor series of 2^f = e^(f ln 2) to the eleventh power (its remainder is below
+// (ln 2 / 2)^12 / 12! = 6.3e-15).  Sixteen instructions; the library's exp takes
+// about three times as many, and these kernels are bound by them.
+__device__ __forceinline__ double pow2(double t) {
+  constexpr double L = 0.69314718055994530942;
+  constexpr double c1 = L, c2 = c1 * L / 2, c3 = c2 * L / 3, c4 = c3 * L / 4, c5 = c4 * L / 5, c6 = c5 * L / 6, c7 = c6 * L / 7,
+                   c8 = c7 * L / 8, c9 = c8 * L / 9, c10 = c9 * L / 10, c11 = c10 * L / 11;
+  t = fmax(t, -1200.0);
+  const double n = rint(t), f = t - n;
+  double p = c11;
+  p = fma(p, f, c10);
+  p = fma(p, f, c9);
+  p = fma(p, f, c8);
+  p = fma(p, f, c7);
+  p = fma(p, f, c6);
+  p = fma(p, f, c5);
+  p = fma(p, f, c4);
+  p = fma(p, f, c3);
+  p = fma(p, f, c2);
+  p = fma(p, f, c1);
+  p = fma(p, f, 1.0);
+  return __builtin_amdgcn_ldexp(p, (int)n);
+}
+
+// log2(r), r > 0: the hardware's float32 logarithm y of the mantissa m, and the
+// rest from m 2^-y = 1 + d with |d| below 2^-20.
+__device__ __forceinline__ double log2_of(double r) {
+  const double m = __builtin_amdgcn_frexp_mant(r);
+  const double y = (double)__builtin_amdgcn_logf((float)m);
+  const double d = fma(m, pow2(-y), -1.0);
+  return (double)__builtin_amdgcn_frexp_exp(r) + y + d * fma(d, fma(d, 1.0 / 3, -0.5), 1.0) * kLog2eD;
+}
+
+// scale_0 exp(z_0 - zmax_0) + ...: the same operations wherever it is evaluated
 template <int NP> __device__ __forceinline__ double mixture(const RowState &r, const float (&z)[NP]) {
-  double m = r.scale[0] * exp((double)z[0] - (double)r.zmax[0]);
+  double m = r.scale[0] * pow2(((double)z[0] - (double)r.zmax[0]) * kLog2eD);
 #pragma unroll
-  for (int j = 1; j < NP; ++j) m = fma(r.scale[j], exp((double)z[j] - (double)r.zmax[j]), m);
+  for (int j = 1; j < NP; ++j) m = fma(r.scale[j], pow2(((double)z[j] - (double)r.zmax[j]) * kLog2eD), m);
   return m;
 }
 
-template <int NP> __device__ __forceinline__ u64 weight(const RowState &r, const float (&z)[NP], int s) {
+// rint(w 2^s) as an integer and as a double
+struct Weight {
+  u64 w;
+  double d;
+};
+template <int NP> __device__ __forceinline__ Weight weight(const RowState &r, const float (&z)[NP], int s) {
   double w;
   if constexpr (NP == 1) {
-    w = r.greedy ? (z[0] == r.zmax[0] ? 1.0 : 0.0) : exp(((double)z[0] - (double)r.zmax[0]) * r.inv_t);
+    w = pow2(((double)z[0] - (double)r.zmax[0]) * (r.inv_t * kLog2eD));
   } else {
-    w = mixture<NP>(r, z) / r.mmax;
-    if (r.greedy) w = w == 1.0 ? 1.0 : 0.0;
-    else if (r.inv_t != 1.0) w = exp(log(w) * r.inv_t);
+    w = mixture<NP>(r, z);
+    if (r.inv_t != 1.0) w = w > 0.0 ? pow2(log2_of(w) * r.inv_t) : 0.0;
   }
-  return (u64)__double2ull_rn(ldexp(w, s));
+  // (w 2^s < 2^52: the sum's last mantissa bit is worth 1, so the addition rounds to an integer)
+  constexpr double kBig = 4503599627370496.0;  // 2^52
+  const double x = fma(w, __builtin_amdgcn_ldexp(1.0, s), kBig);
+  return {(u64)__double_as_longlong(x) & 0xfffffffffffffull, x - kBig};
 }
 
-__device__ __forceinline__ int weight_class(u64 w, int s) {
-  if (w == 0) return kNone;
-  const int msb = 63 - __clzll(w);
-  const int f = msb >= 3 ? (int)(w >> (msb - 3)) & 7 : (int)(w << (3 - msb)) & 7;
-  return min(kLow, (s - msb) * 8 + 7 - f);
+// Class of a weight, from the exponent and first three mantissa bits of the
+// integer as a double.
+__device__ __forceinline__ int weight_class(double d, int s) {
+  const int c = ((1023 + s) << 3) + 7 - (__double2hiint(d) >> 17);
+  return d == 0.0 ? kNone : min(kLow, c);
 }
 // Weights of class c: [lo, hi).
 __device__ __forceinline__ void class_range(int c, int s, u64 &lo, u64 &hi) {
@@ -116,7 +167,6 @@ __device__ __forceinline__ void class_range(int c, int s, u64 &lo, u64 &hi) {
   hi = (u64)(9 + f) << sh;
 }
 
-__device__ __forceinline__ u64 shfl_up64(u64 v, int d) { return __shfl_up(v, d, 64); }
 __device__ __forceinline__ u64 wave_sum64(u64 v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -126,19 +176,16 @@ __device__ __forceinline__ u64 wave_scan64(u64 v) {  // inclusive
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const u64 x = shfl_up64(v, o);
+    const u64 x = __shfl_up(v, o, 64);
     if (lane >= o) v += x;
   }
   return v;
 }
-__device__ __forceinline__ double wave_sum_d(double v) {
+// Sum and maximum over the block (red: 16 doubles; every thread gets the
+// result; fixed order).
+__device__ __forceinline__ double block_sum_d(double v, double *red) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-// (red: 16 doubles; every thread gets the result; fixed order)
-__device__ __forceinline__ double block_sum_d(double v, double *red) {
-  v = wave_sum_d(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -157,28 +204,38 @@ __device__ __forceinline__ double block_max_d(double v, double *red) {
   return t;
 }
 
+// A row's parameters.  The greedy token is the first of the largest weight:
+// a draw with u = 0 among those of weight 2^s.
+__device__ __forceinline__ void set_params(const Args &a, const RowParams &p, int row) {
+  RowState &r = a.w.state[row];
+  const bool greedy = p.t == 0.f;
+  r.greedy = greedy;
+  r.inv_t = greedy ? 1.0 : 1.0 / (double)p.t;
+  r.top_p = p.top_p;
+  r.top_k = p.top_k >= a.V ? 0 : p.top_k;
+  r.cut = !greedy && (r.top_k > 0 || p.top_p < 1.f);
+  const u64 least = greedy ? 1ull << a.s : (u64)__double2ull_rn(ldexp((double)p.min_p, a.s));
+  r.least = least > 1 ? least : 1;
+  const float u = a.u[row];
+  r.u = !greedy && u > 0.f ? fminf(u, 0.99999994f) : 0.f;
+  r.listed = 0;
+}
+
+__global__ __launch_bounds__(kRowsPerCall) void k_sample_params(Args a, ParamBlock pb, int row0) {
+  if (row0 + (int)threadIdx.x < a.rows) set_params(a, pb.r[threadIdx.x], row0 + threadIdx.x);
+}
+
 // Statistics of one tile: each path's maximum and, with several paths, the sum
 // of exponentials; NaN for a tile that holds a NaN or +infinity.
 template <int NP>
-__global__ __launch_bounds__(256) void k_sample_stats(Args a, ParamBlock pb, int row0) {
+__device__ __forceinline__ void tile_stats(const Args &a, int tile, int row) {
   __shared__ float red[16];
   __shared__ double redd[16];
-  const int tile = blockIdx.x, row = row0 + blockIdx.y, t = threadIdx.x;
-  if (tile == 0 && t == 0) {
-    const RowParams p = pb.r[blockIdx.y];
-    RowState &r = a.w.state[row];
-    r.greedy = p.t == 0.f;
-    r.inv_t = p.t == 0.f ? 1.0 : 1.0 / (double)p.t;
-    r.top_p = p.top_p;
-    r.top_k = p.top_k >= a.V ? 0 : p.top_k;
-    r.cut = !r.greedy && (r.top_k > 0 || p.top_p < 1.f);
-    const u64 least = r.greedy ? 1 : __double2ull_rn(ldexp((double)p.min_p, a.s));
-    r.least = least > 1 ? least : 1;
-  }
+  const int t = threadIdx.x;
   float v[NP][8];
 #pragma unroll
   for (int j = 0; j < NP; ++j) {
-    const float *z = path_row<NP>(a, j, row);
+    const float *z = path_row(a, j, row);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int i = tile * kTile + k * 256 + t;
@@ -198,12 +255,17 @@ __global__ __launch_bounds__(256) void k_sample_stats(Args a, ParamBlock pb, int
     double sum = 0.0;
     if (NP > 1 && mx > -INFINITY) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) sum += exp((double)v[j][k] - (double)mx);
+      for (int k = 0; k < 8; ++k) sum += pow2(((double)v[j][k] - (double)mx) * kLog2eD);
     }
     if (bad) sum = __longlong_as_double(0x7ff8000000000000ll);
     sum = block_sum_d(sum, redd);
     if (t == 0) a.w.stats[((size_t)row * a.tiles + tile) * 4 + j] = make_double2(mx, sum);
   }
+}
+template <int NP> __global__ __launch_bounds__(256) void k_sample_stats(Args a) { tile_stats<NP>(a, blockIdx.x, blockIdx.y); }
+template <int NP> __global__ __launch_bounds__(256) void k_sample_stats_params(Args a, ParamBlock pb) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) set_params(a, pb.r[blockIdx.y], blockIdx.y);
+  tile_stats<NP>(a, blockIdx.x, blockIdx.y);
 }
 
 // Row constants: every path's maximum and normaliser, and the largest mixture
@@ -211,82 +273,76 @@ __global__ __launch_bounds__(256) void k_sample_stats(Args a, ParamBlock pb, int
 // the token of a tile's maximum proves lb = max_j of the terms: only tiles with
 // ub >= lb (less a margin over both sides' rounding) are evaluated.
 template <int NP>
-__global__ __launch_bounds__(256) void k_sample_rows(Args a) {
+__global__ __launch_bounds__(kFinal) void k_sample_rows(Args a) {
   __shared__ float red[16];
   __shared__ double redd[16];
   __shared__ int list[kMaxVocab / kTile];
   __shared__ int nlist;
   const int row = blockIdx.x, t = threadIdx.x;
-  const double2 *st = a.w.stats + (size_t)row * a.tiles * 4;
+  static_assert(kMaxVocab / kTile <= kFinal, "one tile per thread");
   RowState &r = a.w.state[row];
+  double2 st[NP];  // this thread's tile
+#pragma unroll
+  for (int j = 0; j < NP; ++j)
+    st[j] = t < a.tiles ? a.w.stats[((size_t)row * a.tiles + t) * 4 + j] : make_double2(-INFINITY, 0.0);
   float M[NP];
-  double S[NP];
+  double S[NP], term[NP];
   bool ok = true;
 #pragma unroll
   for (int j = 0; j < NP; ++j) {
-    float mx = -INFINITY;
-    for (int i = t; i < a.tiles; i += 256) mx = fmaxf(mx, (float)st[i * 4 + j].x);
-    M[j] = block_max(mx, red);
-    double s = 0.0;
-    if (NP == 1)  // (the sums only say whether the row is sound)
-      for (int i = t; i < a.tiles; i += 256) s += st[i * 4 + j].y;
-    else
-      for (int i = t; i < a.tiles; i += 256)
-        if (!(st[i * 4 + j].y == 0.0)) s += st[i * 4 + j].y * exp(st[i * 4 + j].x - (double)M[j]);
-    S[j] = block_sum_d(s, redd);
+    M[j] = block_max((float)st[j].x, red);
+    // (one path: the sums only say whether the row is sound)
+    term[j] = NP > 1 && t < a.tiles ? pow2((st[j].x - (double)M[j]) * kLog2eD) : 0.0;
+    S[j] = block_sum_d(NP > 1 && st[j].y > 0.0 ? st[j].y * term[j] : st[j].y, redd);
     ok = ok && M[j] > -INFINITY && S[j] == S[j];
   }
-  double scale[NP];
-  scale[0] = 1.0;
+  RowState rs;
+  rs.scale[0] = 1.0;
   if (NP > 1) {
     const double al = a.alpha[row];
     ok = ok && al >= 0.0 && al <= 1.0;
-    scale[0] = al / S[0];
+    rs.scale[0] = al / S[0];
 #pragma unroll
-    for (int j = 1; j < NP; ++j) scale[j] = (1.0 - al) / (NP - 1) / S[j];
+    for (int j = 1; j < NP; ++j) rs.scale[j] = (1.0 - al) / (NP - 1) / S[j];
+  }
+#pragma unroll
+  for (int j = 0; j < NP; ++j) rs.zmax[j] = M[j];
+  double mmax = 1.0;
+  if (NP > 1 && ok) {
+    double lb = 0.0, ub = 0.0;
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      term[j] *= rs.scale[j];
+      lb = fmax(lb, term[j]);
+      ub += term[j];
+    }
+    if (t == 0) nlist = 0;
+    lb = block_max_d(lb, redd) * (1.0 - 1e-9);  // (its barriers come after the clearing)
+    if (t < a.tiles && ub >= lb) list[atomicAdd(&nlist, 1)] = t;  // (a maximum has no order)
+    __syncthreads();
+    double mx = 0.0;
+    for (int n = 0; n < nlist; ++n) {
+      float z[kTile / kFinal][NP];
+#pragma unroll
+      for (int k = 0; k < kTile / kFinal; ++k)
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+          const int i = list[n] * kTile + k * kFinal + t;
+          z[k][j] = i < a.V ? path_row(a, j, row)[i] : -INFINITY;
+        }
+#pragma unroll
+      for (int k = 0; k < kTile / kFinal; ++k) mx = fmax(mx, mixture<NP>(rs, z[k]));
+    }
+    mmax = block_max_d(mx, redd);
   }
   if (t == 0) {
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-      r.scale[j] = scale[j];
+      r.scale[j] = rs.scale[j] / mmax;
       r.zmax[j] = M[j];
     }
-    const float u = a.u[row];
-    r.u = u > 0.f ? fminf(u, 0.99999994f) : 0.f;
     r.valid = ok;
-    r.mmax = 1.0;
-    nlist = 0;
   }
-  if (NP == 1 || !ok) return;
-  auto term = [&](int i, int j) { return scale[j] * exp(st[i * 4 + j].x - (double)M[j]); };
-  double lb = 0.0;
-  for (int i = t; i < a.tiles; i += 256)
-#pragma unroll
-    for (int j = 0; j < NP; ++j) lb = fmax(lb, term(i, j));
-  lb = block_max_d(lb, redd) * (1.0 - 1e-9);  // (nlist is cleared by this barrier)
-  for (int i = t; i < a.tiles; i += 256) {
-    double ub = 0.0;
-#pragma unroll
-    for (int j = 0; j < NP; ++j) ub += term(i, j);
-    if (ub >= lb) list[atomicAdd(&nlist, 1)] = i;  // (the order does not matter to a maximum)
-  }
-  __syncthreads();
-  RowState rs;
-#pragma unroll
-  for (int j = 0; j < NP; ++j) {
-    rs.scale[j] = scale[j];
-    rs.zmax[j] = M[j];
-  }
-  double mx = 0.0;
-  for (int n = 0; n < nlist; ++n)
-    for (int i = list[n] * kTile + t; i < min(a.V, (list[n] + 1) * kTile); i += 256) {
-      float z[NP];
-#pragma unroll
-      for (int j = 0; j < NP; ++j) z[j] = path_row<NP>(a, j, row)[i];
-      mx = fmax(mx, mixture<NP>(rs, z));
-    }
-  mx = block_max_d(mx, redd);
-  if (t == 0) r.mmax = mx;
 }
 
 // Weights of one part of a row: histogram by class and the tokens' classes, or,
@@ -304,63 +360,73 @@ __global__ __launch_bounds__(256) void k_sample_weigh(Args a) {
   __syncthreads();
   u64 kept = 0;  // no cut: kept mass; cut: mass of the low class
   unsigned low = 0;
-  for (int i = lo + t; i < hi; i += 256) {
-    float z[NP];
+  for (int i0 = lo; i0 < hi; i0 += 1024) {
+    float z[4][NP];
 #pragma unroll
-    for (int j = 0; j < NP; ++j) z[j] = path_row<NP>(a, j, row)[i];
-    const u64 w = weight<NP>(r, z, a.s);
-    if (!r.cut) {
-      if (w >= r.least) kept += w;
-      continue;
-    }
-    const int c = weight_class(w, a.s);
-    a.w.cls[(size_t)row * a.V + i] = (uint8_t)c;
-    if (c == kLow) {
-      kept += w;
-      ++low;
-    } else if (c < kLow) {
-      atomicAdd(&mass[c], w);
-      atomicAdd(&count[c], 1u);
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < NP; ++j) z[k][j] = path_row(a, j, row)[min(i0 + k * 256 + t, hi - 1)];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + k * 256 + t;
+      if (i >= hi) break;
+      const Weight w = weight<NP>(r, z[k], a.s);
+      if (!r.cut) {
+        if (w.w >= r.least) kept += w.w;
+        continue;
+      }
+      const int c = weight_class(w.d, a.s);
+      a.w.cls[(size_t)row * a.Vp + i] = (uint8_t)c;
+      if (c == kLow) {
+        kept += w.w;
+        ++low;
+      } else if (c < kLow) {
+        atomicAdd(&mass[c], w.w);
+        if (r.top_k > 0) atomicAdd(&count[c], 1u);
+      }
     }
   }
   const int slot = r.cut ? kLow : 0;
   kept = wave_sum64(kept);
-  if ((t & 63) == 0) atomicAdd(&mass[slot], kept);
   const u64 lows = wave_sum64(low);
-  if ((t & 63) == 0) atomicAdd(&count[slot], (unsigned)lows);
+  if ((t & 63) == 0) {
+    atomicAdd(&mass[slot], kept);
+    atomicAdd(&count[slot], (unsigned)lows);
+  }
   __syncthreads();
   const size_t o = ((size_t)row * a.parts + part) * kClasses + t;
   if (r.cut) {
     a.w.tmass[o] = mass[t];
-    a.w.tcount[o] = count[t];
+    if (r.top_k > 0) a.w.tcount[o] = count[t];
   } else if (t == 0) {
     a.w.tmass[o] = mass[0];
   }
 }
 
-// The class in which the cut falls, and where each part's tokens go in the list.
+// Where the cuts can fall: the class in which top-k is reached, and those in
+// which top-p can be, whose target follows from what top-k keeps of its class.
 __global__ __launch_bounds__(256) void k_sample_cut(Args a) {
   __shared__ u64 ms[kClasses], red[4];
   __shared__ unsigned cs[kClasses], wred[4];
-  __shared__ int last_s;
+  __shared__ int kc_s, pl_s, ph_s;
   const int row = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6;
   RowState &r = a.w.state[row];
   if (!r.valid || !r.cut) return;
+  const int top_k = r.top_k;
   u64 m = 0;
   unsigned c = 0;
-  for (int p = 0; p < a.parts; ++p) {
-    const size_t o = ((size_t)row * a.parts + p) * kClasses + t;
-    m += a.w.tmass[o];
-    c += a.w.tcount[o];
-  }
-  a.w.mass[(size_t)row * kClasses + t] = m;
-  a.w.count[(size_t)row * kClasses + t] = c;
+  const size_t o = (size_t)row * a.parts * kClasses + t;
+#pragma unroll 8
+  for (int p = 0; p < a.parts; ++p) m += a.w.tmass[o + (size_t)p * kClasses];
+  if (top_k > 0)
+#pragma unroll 8
+    for (int p = 0; p < a.parts; ++p) c += a.w.tcount[o + (size_t)p * kClasses];
   const u64 mi = wave_scan64(m), ci = wave_scan64(c);
   if (lane == 63) {
     red[wave] = mi;
     wred[wave] = (unsigned)ci;
   }
-  if (t == 0) last_s = kLow;
+  if (t == 0) kc_s = pl_s = ph_s = -1;
   __syncthreads();
   u64 mo = 0, total = 0;
   unsigned co = 0;
@@ -373,72 +439,84 @@ __global__ __launch_bounds__(256) void k_sample_cut(Args a) {
   }
   ms[t] = mo + mi;
   cs[t] = co + (unsigned)ci;
+  a.w.upto[(size_t)row * kClasses + t] = ms[t];
   __syncthreads();
-  // the first class at which top-k, or without it top-p, is reached
-  bool at;
-  if (r.top_k > 0) {
-    at = cs[t] >= (unsigned)r.top_k && (t == 0 || cs[t - 1] < (unsigned)r.top_k);
-  } else {
-    const u64 need = (u64)ceil((double)r.top_p * (double)total);
-    at = ms[t] >= need && (t == 0 || ms[t - 1] < need);
+  const u64 m0 = t ? ms[t - 1] : 0;
+  const unsigned c0 = t ? cs[t - 1] : 0;
+  if (top_k > 0 && cs[t] >= (unsigned)top_k && c0 < (unsigned)top_k) kc_s = t;
+  __syncthreads();
+  const int kc = kc_s;
+  // least and largest mass that top-k can keep
+  u64 wl = total, wh = total;
+  unsigned need = 0;
+  bool whole = false;
+  if (kc >= 0) {
+    need = (unsigned)top_k - (kc ? cs[kc - 1] : 0);
+    const u64 before = kc ? ms[kc - 1] : 0, in = ms[kc] - before;
+    whole = cs[kc] == (unsigned)top_k;
+    u64 lo, hi;
+    class_range(kc, a.s, lo, hi);
+    wl = whole ? ms[kc] : before + need * lo;
+    wh = whole ? ms[kc] : before + min(in, need * (hi - 1));
   }
-  if (at) last_s = min(t, kLow);
+  const float top_p = r.top_p;
+  if (top_p < 1.f) {
+    auto reach = [&](u64 w) {
+      const u64 x = (u64)ceil((double)top_p * (double)w);
+      return x < 1 ? 1 : x > w ? w : x;
+    };
+    const u64 nl = reach(wl), nh = reach(wh);
+    if (ms[t] >= nl && m0 < nl) pl_s = t;
+    if (ms[t] >= nh && m0 < nh) ph_s = t;
+  }
   __syncthreads();
-  const int last = last_s;
   if (t == 0) {
-    r.last = last;
-    r.listed = (int)cs[last];
-  }
-  // tokens each part lists, then the exclusive sums over the parts
-  unsigned *toff = a.w.toff + (size_t)row * a.parts;
-  for (int p = wave; p < a.parts; p += 4) {
-    const unsigned *tc = a.w.tcount + ((size_t)row * a.parts + p) * kClasses;
-    u64 n = 0;
-    for (int k = lane; k <= last; k += 64) n += tc[k];
-    n = wave_sum64(n);
-    if (lane == 0) toff[p] = (unsigned)n;
-  }
-  __syncthreads();
-  if (wave == 0) {
-    unsigned before = 0;
-    for (int p0 = 0; p0 < a.parts; p0 += 64) {
-      const unsigned n = p0 + lane < a.parts ? toff[p0 + lane] : 0;
-      const unsigned incl = (unsigned)wave_scan64(n);
-      if (p0 + lane < a.parts) toff[p0 + lane] = before + incl - n;
-      before += __shfl(incl, 63, 64);
-    }
+    r.kc = kc;
+    r.k_need = (int)need;
+    r.k_whole = whole;
+    r.k_mass = kc > 0 ? ms[kc - 1] : 0;
+    r.pl = top_p < 1.f ? pl_s : 0;
+    r.ph = top_p < 1.f ? ph_s : -1;
+    r.lc = r.least > 1 ? weight_class((double)r.least, a.s) : -1;
   }
 }
 
-// Tokens of the classes up to the cut's, in index order, with their weights.
+// Tokens of those classes, with their weights, in any order.
 template <int NP>
 __global__ __launch_bounds__(256) void k_sample_list(Args a) {
-  __shared__ unsigned wn[4];
-  const int part = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ int idx[4096];
+  __shared__ unsigned n_s, at_s;
+  const int part = blockIdx.x, row = blockIdx.y, t = threadIdx.x;
   const RowState r = a.w.state[row];
   if (!r.valid || !r.cut) return;
+  const int kc = r.k_whole ? -1 : r.kc;
   const int lo = part * a.part, hi = min(a.V, lo + a.part);
-  const int q = (a.part + 3) / 4, w0 = lo + wave * q, w1 = min(hi, w0 + q);  // a wave's tokens
-  const uint8_t *cls = a.w.cls + (size_t)row * a.V;
-  unsigned n = 0;
-  for (int i = w0; i < w1; i += 64) n += __popcll(__ballot(i + lane < w1 && cls[min(i + lane, w1 - 1)] <= r.last));
-  if (lane == 0) wn[wave] = n;
-  __syncthreads();
-  if (n == 0) return;
-  size_t at = (size_t)row * a.V + a.w.toff[(size_t)row * a.parts + part];
-  for (int w = 0; w < wave; ++w) at += wn[w];
-  for (int i = w0; i < w1; i += 64) {
-    const bool in = i + lane < w1 && cls[min(i + lane, w1 - 1)] <= r.last;
-    const u64 all = __ballot(in);
-    if (in) {
+  const uint8_t *cls = a.w.cls + (size_t)row * a.Vp;
+  for (int i0 = lo; i0 < hi; i0 += 4096) {
+    if (t == 0) n_s = 0;
+    __syncthreads();
+    const int i = i0 + t * 16;
+    if (i < hi) {
+      const u32x4 v = *(const u32x4 *)(cls + i);
+#pragma unroll
+      for (int b = 0; b < 16; ++b) {
+        const int c = (v[b >> 2] >> (8 * (b & 3))) & 0xff;
+        if (((c >= r.pl && c <= r.ph) || c == kc || c == r.lc) && c <= kLow && i + b < hi) idx[atomicAdd(&n_s, 1u)] = i + b;
+      }
+    }
+    __syncthreads();
+    const unsigned n = n_s;
+    if (t == 0 && n) at_s = atomicAdd(&a.w.state[row].listed, n);
+    __syncthreads();
+    for (unsigned k = t; k < n; k += 256) {
       float z[NP];
 #pragma unroll
-      for (int j = 0; j < NP; ++j) z[j] = path_row<NP>(a, j, row)[i + lane];
-      const size_t o = at + __popcll(all & ((1ull << lane) - 1));
-      a.w.lw[o] = weight<NP>(r, z, a.s);
-      a.w.li[o] = i + lane;
+      for (int j = 0; j < NP; ++j) z[j] = path_row(a, j, row)[idx[k]];
+      const size_t o = (size_t)row * a.V + at_s + k;
+      a.w.lw[o] = weight<NP>(r, z, a.s).w;
+      a.w.li[o] = idx[k];
     }
-    at += __popcll(all);
+    __syncthreads();
   }
 }
 
@@ -447,52 +525,75 @@ struct FinalShared {
   unsigned count[256];
   u64 rw[kRankCap];
   int ri[kRankCap];
+  u64 pmass[kMaxParts];
   u64 red[kFinal / 64];
-  u64 cut_w, sum, lo, hi, need;
-  int cut_i, n, found;
+  u64 cut_w, sum, need;
+  int cut_i, n, bin, token;
   unsigned inside;
 };
 
-// The index of the n-th (from 0) entry with lw == w of a list in index order.
-__device__ int nth_equal(FinalShared &sh, const u64 *lw, const int *li, int n, u64 w, unsigned nth) {
-  constexpr int NW = kFinal / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int seg = (n + NW - 1) / NW, s0 = wave * seg, s1 = min(n, s0 + seg);
-  unsigned c = 0;
-  for (int i = s0; i < s1; i += 64) c += __popcll(__ballot(i + lane < s1 && lw[min(i + lane, n - 1)] == w));
-  __syncthreads();
-  if (lane == 0) sh.red[wave] = c;
-  __syncthreads();
-  u64 before = 0;
-  for (int k = 0; k < wave; ++k) before += sh.red[k];
-  if (before <= nth && nth < before + c) {
-    for (int i = s0; i < s1; i += 64) {
-      const u64 all = __ballot(i + lane < s1 && lw[min(i + lane, n - 1)] == w);
-      const int k = __popcll(all);
-      if (before + k > nth) {
-        const int mine = __popcll(all & ((1ull << lane) - 1));
-        if (((all >> lane) & 1) && before + mine == nth) sh.cut_i = li[i + lane];
-        break;
+// One step of narrowing: of 256 bins (filled in sh.mass, sh.count), taken from
+// the first in `descending` or ascending order, the one in which `need` (of mass or
+// number) is reached: sh.bin, sh.inside, what is left of need in sh.need, the
+// mass of the bins before it in sh.sum.  By the first wave.
+__device__ __forceinline__ void pick_bin(FinalShared &sh, u64 need, bool by_mass, bool descending) {
+  const int lane = threadIdx.x & 63;
+  u64 v[4], m[4], vs = 0, msum = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int b = descending ? 255 - (lane * 4 + k) : lane * 4 + k;
+    m[k] = sh.mass[b];
+    v[k] = by_mass ? m[k] : sh.count[b];
+    vs += v[k];
+    msum += m[k];
+  }
+  u64 before = wave_scan64(vs), mb = wave_scan64(msum) - msum;
+  need = min(need, __shfl(before, 63, 64));
+  before -= vs;
+  if (before < need && before + vs >= need) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (before < need && before + v[k] >= need) {
+        const int b = descending ? 255 - (lane * 4 + k) : lane * 4 + k;
+        sh.bin = b;
+        sh.inside = sh.count[b];
+        sh.need = need - before;
+        sh.sum = mb;
       }
-      before += k;
+      before += v[k];
+      mb += m[k];
     }
   }
-  __syncthreads();
-  return sh.cut_i;
 }
 
-// Where the order by (weight falling, index) is cut inside the class [lo, hi)
-// of the list, after `need` of its tokens (by_mass: after the shortest run
-// whose mass reaches need; the class holds as much): the last token that stays
-// in sh.cut_w, sh.cut_i, the mass that stays of the class in sh.sum.  Classes of
-// more than kRankCap tokens are narrowed 256-fold, by the same histogram,
-// until few are left or all are equal.
-__device__ void cut_class(FinalShared &sh, const u64 *lw, const int *li, int n, u64 lo, u64 hi, unsigned inside,
-                          u64 need, bool by_mass) {
+// Where the order by (weight falling, index) is cut among the listed weights of
+// [lo, hi), `inside` of them, after `need` tokens (by_mass: after the shortest run
+// whose mass reaches need; the range holds as much): the last token that stays
+// in sh.cut_w, sh.cut_i, the mass that stays of the range in sh.sum.  Ranges of
+// more than kRankCap tokens are narrowed 256-fold by histograms of the weight and, once all
+// weights are equal, of the index.
+__device__ void cut_range(FinalShared &sh, const u64 *lw, const int *li, int n, int V, u64 lo, u64 hi, u64 need, bool by_mass) {
   const int t = threadIdx.x;
-  u64 above = 0;  // mass of the class above the narrowed range
-  while (inside > kRankCap && hi - lo > 1) {
-    const int bits = 64 - __clzll(hi - lo - 1), shift = bits > 8 ? bits - 8 : 0;
+  u64 above = 0;  // mass that stays above the narrowed range
+  int ilo = 0, ihi = V;
+  unsigned inside = 0;
+  {
+    unsigned mine = 0;
+    for (int i = t; i < n; i += kFinal) mine += lw[i] >= lo && lw[i] < hi;
+    const u64 w = wave_sum64(mine);
+    __syncthreads();
+    if ((t & 63) == 0) sh.red[t >> 6] = w;
+    __syncthreads();
+    for (int k = 0; k < kFinal / 64; ++k) inside += (unsigned)sh.red[k];
+  }
+  while (inside > kRankCap && (hi - lo > 1 || ihi - ilo > 1)) {
+    const bool by_index = hi - lo <= 1;
+    const u64 width = by_index ? ihi - ilo : hi - lo;
+    const int bits = 64 - __clzll(width - 1), shift = bits > 8 ? bits - 8 : 0;
+    if (by_index && by_mass) {  // (equal weights: so many of them)
+      need = (need + lo - 1) / lo;
+      by_mass = false;
+    }
     __syncthreads();
     if (t < 256) {
       sh.mass[t] = 0;
@@ -501,63 +602,49 @@ __device__ void cut_class(FinalShared &sh, const u64 *lw, const int *li, int n, 
     __syncthreads();
     for (int i = t; i < n; i += kFinal) {
       const u64 w = lw[i];
-      if (w >= lo && w < hi) {
-        const int b = (int)((w - lo) >> shift);
-        atomicAdd(&sh.mass[b], w);
-        atomicAdd(&sh.count[b], 1u);
-      }
+      const int ix = li[i];
+      if (w < lo || w >= hi || ix < ilo || ix >= ihi) continue;
+      const int b = by_index ? (ix - ilo) >> shift : (int)((w - lo) >> shift);
+      atomicAdd(&sh.mass[b], w);
+      atomicAdd(&sh.count[b], 1u);
     }
     __syncthreads();
-    if (t == 0) {
-      u64 left = need, ab = 0;
-      int b = 255;
-      for (;; --b) {
-        const u64 have = by_mass ? sh.mass[b] : sh.count[b];
-        if (have >= left || b == 0) break;
-        left -= have;
-        ab += sh.mass[b];
-      }
-      sh.lo = lo + ((u64)b << shift);
-      sh.hi = sh.lo + (1ull << shift);
-      sh.need = left;
-      sh.sum = ab;
-      sh.inside = sh.count[b];
-    }
+    if (t < 64) pick_bin(sh, need, by_mass, !by_index);
     __syncthreads();
-    lo = sh.lo;
-    hi = sh.hi < hi ? sh.hi : hi;
+    if (by_index) {
+      ilo += sh.bin << shift;
+      ihi = min(ihi, ilo + (1 << shift));
+    } else {
+      lo += (u64)sh.bin << shift;
+      hi = min(hi, lo + (1ull << shift));
+    }
     need = sh.need;
     above += sh.sum;
     inside = sh.inside;
   }
   __syncthreads();
-  if (inside > kRankCap) {  // equal weights: by index
-    const u64 nth = by_mass ? (need + lo - 1) / lo : need;
-    nth_equal(sh, lw, li, n, lo, (unsigned)nth - 1);
-    if (t == 0) {
-      sh.cut_w = lo;
-      sh.sum = above + nth * lo;
-    }
-    __syncthreads();
-    return;
-  }
   if (t == 0) sh.n = 0;
   __syncthreads();
   for (int i = t; i < n; i += kFinal) {
     const u64 w = lw[i];
-    if (w >= lo && w < hi) {
-      const int k = atomicAdd(&sh.n, 1);  // (any order: ranks come from weight and index)
-      if (k < kRankCap) {
-        sh.rw[k] = w;
-        sh.ri[k] = li[i];
-      }
+    const int ix = li[i];
+    if (w < lo || w >= hi || ix < ilo || ix >= ihi) continue;
+    const int k = atomicAdd(&sh.n, 1);  // (any order: ranks come from weight and index)
+    if (k < kRankCap) {
+      sh.rw[k] = w;
+      sh.ri[k] = ix;
     }
+  }
+  if (t == 0) {
+    sh.cut_w = lo;
+    sh.cut_i = V;
+    sh.sum = above;
   }
   __syncthreads();
   const int k = min(sh.n, kRankCap);
-  for (int e = t; e < k; e += kFinal) {
-    const u64 w = sh.rw[e];
-    const int ix = sh.ri[e];
+  if (t < k) {
+    const u64 w = sh.rw[t];
+    const int ix = sh.ri[t];
     u64 mass = 0;
     unsigned rank = 0;
     for (int o = 0; o < k; ++o)
@@ -576,162 +663,158 @@ __device__ void cut_class(FinalShared &sh, const u64 *lw, const int *li, int n, 
   __syncthreads();
 }
 
-// The first of n entries, in order, whose running sum of `get` exceeds u times
-// their whole sum, and its share of it.  get(i): the entry's weight, 0 where
-// it does not stay.
-template <typename F>
-__device__ void draw(FinalShared &sh, int n, float u, F get, int &found, double &share) {
+// One workgroup per row: the exact cut among the listed tokens, every part's
+// mass above it, the part in which the draw falls, its token.
+template <int NP>
+__global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
   constexpr int NW = kFinal / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int seg = ((n + NW - 1) / NW + 63) / 64 * 64, s0 = min(n, wave * seg), s1 = min(n, s0 + seg);
-  u64 sum = 0;
-  for (int i = s0 + lane; i < s1; i += 64) sum += get(i);
-  sum = wave_sum64(sum);
+  __shared__ FinalShared sh;
+  const int row = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const RowState r = a.w.state[row];
+  if (!r.valid) {
+    if (t == 0) {
+      a.token[row] = -1;
+      if (a.prob) a.prob[row] = 0.f;
+    }
+    return;
+  }
+  const u64 *lw = a.w.lw + (size_t)row * a.V;
+  const int *li = a.w.li + (size_t)row * a.V;
+  const u64 *tm = a.w.tmass + (size_t)row * a.parts * kClasses;
+  // stays: W > cut_w, or W == cut_w and the index at most cut_i
+  u64 cut_w = 1;
+  int cut_i = a.V;
+  if (r.cut) {
+    const u64 *upto = a.w.upto + (size_t)row * kClasses;
+    u64 total = upto[kLow], lo, hi;
+    if (r.kc >= 0) {
+      class_range(r.kc, a.s, lo, hi);
+      if (r.k_whole) {
+        total = upto[r.kc];
+        cut_w = lo;
+      } else {
+        cut_range(sh, lw, li, r.listed, a.V, lo, hi, r.k_need, false);
+        total = r.k_mass + sh.sum;
+        cut_w = sh.cut_w;
+        cut_i = sh.cut_i;
+      }
+    }
+    if (r.top_p < 1.f) {
+      u64 need = (u64)ceil((double)r.top_p * (double)total);
+      need = need < 1 ? 1 : need > total ? total : need;
+      int c = r.pl;
+      while (c < r.ph && upto[c] < need) ++c;
+      class_range(c, a.s, lo, hi);
+      __syncthreads();
+      cut_range(sh, lw, li, r.listed, a.V, lo, hi, need - (c ? upto[c - 1] : 0), true);
+      cut_w = sh.cut_w;
+      cut_i = sh.cut_i;
+    }
+  }
+  if (r.least > cut_w) {
+    cut_w = r.least;
+    cut_i = a.V;
+  }
+  // the parts' masses: the classes above the cut's from their histograms, and
+  // what stays of that class from the list
+  if (r.cut) {
+    const int ce = weight_class((double)cut_w, a.s);
+    u64 lo, hi;
+    class_range(ce, a.s, lo, hi);
+    const bool whole = cut_w <= lo && cut_i >= a.V - 1;
+    const int last = whole ? ce : ce - 1;
+    for (int p = wave; p < a.parts; p += NW) {
+      u64 m = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = k * 64 + lane;
+        const u64 x = tm[(size_t)p * kClasses + c];
+        m += c <= last ? x : 0;
+      }
+      m = wave_sum64(m);
+      if (lane == 0) sh.pmass[p] = m;
+    }
+    __syncthreads();
+    if (!whole)
+      for (int i = t; i < (int)r.listed; i += kFinal) {
+        const u64 w = lw[i];
+        if (w < hi && (w > cut_w || (w == cut_w && li[i] <= cut_i))) atomicAdd(&sh.pmass[li[i] / a.part], w);
+      }
+  } else {
+    for (int p = t; p < a.parts; p += kFinal) sh.pmass[p] = tm[(size_t)p * kClasses];
+  }
   __syncthreads();
-  if (lane == 0) sh.red[wave] = sum;
-  if (threadIdx.x == 0) sh.found = -1;
+  static_assert(kMaxParts <= kFinal, "one part per thread");
+  u64 m = t < a.parts ? sh.pmass[t] : 0;
+  u64 incl = wave_scan64(m);
+  if (lane == 63) sh.red[wave] = incl;
   __syncthreads();
   u64 total = 0, before = 0;
   for (int k = 0; k < NW; ++k) {
     if (k < wave) before += sh.red[k];
     total += sh.red[k];
   }
-  u64 target = (u64)((double)u * (double)total);
-  if (total && target >= total) target = total - 1;
-  if (sum && before <= target && target < before + sum) {
+  if (total == 0) {  // (not reached: the largest weight stays)
+    if (t == 0) {
+      a.token[row] = -1;
+      if (a.prob) a.prob[row] = 0.f;
+    }
+    return;
+  }
+  incl += before;
+  u64 target = (u64)((double)r.u * (double)total);
+  if (target >= total) target = total - 1;
+  if (target < incl && target >= incl - m) {
+    sh.bin = t;
+    sh.sum = incl - m;
+  }
+  __syncthreads();
+  // the token: each wave sums a run of the part, the one that holds the target scans it
+  const int p0 = sh.bin * a.part, n = min(a.V, p0 + a.part) - p0;
+  before = sh.sum;
+  auto get = [&](int i) __attribute__((always_inline)) {
+    float z[NP];
+#pragma unroll
+    for (int j = 0; j < NP; ++j) z[j] = path_row(a, j, row)[p0 + min(i, n - 1)];
+    const u64 w = weight<NP>(r, z, a.s).w;
+    return i < n && (w > cut_w || (w == cut_w && p0 + i <= cut_i)) ? w : 0;
+  };
+  const int seg = ((n + NW - 1) / NW + 63) / 64 * 64, s0 = wave * seg, s1 = min(n, s0 + seg);
+  u64 sum = 0;
+#pragma unroll 4
+  for (int i = s0; i < s1; i += 64) sum += get(i + lane);
+  sum = wave_sum64(sum);
+  if (lane == 0) sh.red[wave] = sum;
+  __syncthreads();
+  for (int k = 0; k < wave; ++k) before += sh.red[k];
+  if (before <= target && target < before + sum)
     for (int i = s0; i < s1; i += 64) {
-      const u64 w = i + lane < s1 ? get(i + lane) : 0;
-      const u64 incl = before + wave_scan64(w);
-      const u64 hit = __ballot(incl > target);
+      const u64 w = get(i + lane), upto_i = before + wave_scan64(w);
+      const u64 hit = __ballot(upto_i > target);
       if (hit) {
         if (lane == __ffsll(hit) - 1) {
-          sh.found = i + lane;
-          sh.sum = w;
+          a.token[row] = p0 + i + lane;
+          if (a.prob) a.prob[row] = r.greedy ? 1.f : (float)((double)w / (double)total);
         }
         break;
       }
-      before = __shfl(incl, 63, 64);
+      before = __shfl(upto_i, 63, 64);
     }
-  }
-  __syncthreads();
-  found = sh.found;
-  share = found < 0 ? 0.0 : (double)sh.sum / (double)total;
-}
-
-// One workgroup per row: the exact cut in its class, then the draw.
-template <int NP>
-__global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
-  __shared__ FinalShared sh;
-  const int row = blockIdx.x, t = threadIdx.x;
-  const RowState r = a.w.state[row];
-  int token = -1;
-  double share = 0.0;
-  if (r.valid && !r.cut) {
-    // the part in which the draw falls, then its token
-    const u64 *tm = a.w.tmass + (size_t)row * a.parts * kClasses;
-    int part;
-    u64 total = 0, before = 0;
-    for (int p = 0; p < a.parts; ++p) total += tm[(size_t)p * kClasses];
-    const float u = r.greedy ? 0.f : r.u;
-    u64 target = (u64)((double)u * (double)total);
-    if (target >= total) target = total - 1;
-    for (part = 0; part < a.parts - 1; ++part) {
-      const u64 m = tm[(size_t)part * kClasses];
-      if (target < before + m) break;
-      before += m;
-    }
-    const int lo = part * a.part, hi = min(a.V, lo + a.part);
-    auto get = [&](int i) {
-      float z[NP];
-#pragma unroll
-      for (int j = 0; j < NP; ++j) z[j] = path_row<NP>(a, j, row)[lo + i];
-      const u64 w = weight<NP>(r, z, a.s);
-      return w >= r.least ? w : 0;
-    };
-    constexpr int NW = kFinal / 64;
-    const int lane = t & 63, wave = t >> 6, n = hi - lo;
-    const int seg = ((n + NW - 1) / NW + 63) / 64 * 64, s0 = min(n, wave * seg), s1 = min(n, s0 + seg);
-    u64 sum = 0;
-    for (int i = s0 + lane; i < s1; i += 64) sum += get(i);
-    sum = wave_sum64(sum);
-    if (lane == 0) sh.red[wave] = sum;
-    __syncthreads();
-    for (int k = 0; k < wave; ++k) before += sh.red[k];
-    if (before <= target && target < before + sum)
-      for (int i = s0; i < s1; i += 64) {
-        const u64 w = i + lane < s1 ? get(i + lane) : 0;
-        const u64 incl = before + wave_scan64(w);
-        const u64 hit = __ballot(incl > target);
-        if (hit) {
-          if (lane == __ffsll(hit) - 1) {
-            a.token[row] = lo + i + lane;
-            if (a.prob) a.prob[row] = r.greedy ? 1.f : (float)((double)w / (double)total);
-          }
-          break;
-        }
-        before = __shfl(incl, 63, 64);
-      }
-    return;
-  }
-  if (r.valid) {
-    const u64 *lw = a.w.lw + (size_t)row * a.V;
-    const int *li = a.w.li + (size_t)row * a.V;
-    const u64 *mass = a.w.mass + (size_t)row * kClasses;
-    const unsigned *count = a.w.count + (size_t)row * kClasses;
-    u64 total = 0;           // mass of the tokens that top-k keeps
-    u64 cut_w = 0;
-    int cut_i = a.V;         // stays: (W > cut_w) or (W == cut_w and index <= cut_i)
-    u64 lo, hi;
-    if (r.top_k > 0 && (unsigned)r.listed > (unsigned)r.top_k) {
-      unsigned before = 0;
-      for (int c = 0; c < r.last; ++c) {
-        before += count[c];
-        total += mass[c];
-      }
-      class_range(r.last, a.s, lo, hi);
-      cut_class(sh, lw, li, r.listed, lo, hi, count[r.last], (u64)r.top_k - before, false);
-      total += sh.sum;
-      cut_w = sh.cut_w;
-      cut_i = sh.cut_i;
-    } else {
-      for (int c = 0; c <= (r.top_k > 0 ? r.last : kLow); ++c) total += mass[c];
-    }
-    if (r.top_p < 1.f) {
-      u64 need = (u64)ceil((double)r.top_p * (double)total), before = 0;
-      need = need < 1 ? 1 : need > total ? total : need;
-      int c = 0;
-      for (; c < r.last && before + mass[c] < need; ++c) before += mass[c];
-      class_range(c, a.s, lo, hi);
-      __syncthreads();
-      cut_class(sh, lw, li, r.listed, lo, hi, count[c], need - before, true);
-      cut_w = sh.cut_w;
-      cut_i = sh.cut_i;
-    }
-    int at;
-    draw(sh, r.listed, r.u, [&](int i) {
-      const u64 w = lw[i];
-      return w >= r.least && (w > cut_w || (w == cut_w && li[i] <= cut_i)) ? w : 0;
-    }, at, share);
-    token = at < 0 ? -1 : li[at];
-  }
-  if (t == 0) {
-    a.token[row] = token;
-    if (a.prob) a.prob[row] = (float)share;
-  }
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Parts of a row: statistics tiles, several of them together where the rows
-// alone fill the chip (a part writes 3 KB of histogram, which the next kernel
-// reads).
+// Parts of a row: statistics tiles, up to four of them together where the rows
+// alone fill the chip (a part's histogram is written and read again: 3 KB).
 void partition(int rows, int vocab, int *tiles, int *parts, int *part) {
   *tiles = (vocab + kTile - 1) / kTile;
   int f = 1;
-  while (f < 8 && (long long)rows * ((*tiles + f) / (f + 1)) >= 1024) ++f;
+  while (f < 4 && (long long)rows * ((*tiles + f) / (f + 1)) >= 1024) ++f;
   *part = f * kTile;
   *parts = (vocab + *part - 1) / *part;
 }
+
+int round16(int x) { return (x + 15) / 16 * 16; }
 
 size_t layout(int rows, int vocab, char *base, Work *w) {
   int tiles, parts, part;
@@ -748,10 +831,8 @@ size_t layout(int rows, int vocab, char *base, Work *w) {
   x.stats = (double2 *)take(R * tiles * 4 * sizeof(double2));
   x.tmass = (u64 *)take(R * parts * kClasses * 8);
   x.tcount = (unsigned *)take(R * parts * kClasses * 4);
-  x.mass = (u64 *)take(R * kClasses * 8);
-  x.count = (unsigned *)take(R * kClasses * 4);
-  x.toff = (unsigned *)take(R * parts * 4);
-  x.cls = (uint8_t *)take(R * V);
+  x.upto = (u64 *)take(R * kClasses * 8);
+  x.cls = (uint8_t *)take(R * round16(vocab));
   x.lw = (u64 *)take(R * V * 8);
   x.li = (int *)take(R * V * 4);
   if (w) *w = x;
@@ -766,10 +847,17 @@ template <int NP> hipError_t launch(const Args &a, const dbt_sampling *p, bool c
     const int n = a.rows - r0 < kRowsPerCall ? a.rows - r0 : kRowsPerCall;
     for (int i = 0; i < n; ++i)
       pb.r[i] = RowParams{p[r0 + i].temperature, p[r0 + i].top_p, p[r0 + i].min_p, p[r0 + i].top_k};
-    hipLaunchKernelGGL(k_sample_stats<NP>, dim3(a.tiles, n), dim3(256), 0, st, a, pb, r0);
+    if (a.rows <= kRowsPerCall)  // (a launch fewer)
+      hipLaunchKernelGGL(k_sample_stats_params<NP>, dim3(a.tiles, n), dim3(256), 0, st, a, pb);
+    else
+      hipLaunchKernelGGL(k_sample_params, dim3(1), dim3(kRowsPerCall), 0, st, a, pb, r0);
     if (const hipError_t e = hipGetLastError()) return e;
   }
-  hipLaunchKernelGGL(k_sample_rows<NP>, dim3(a.rows), dim3(256), 0, st, a);
+  if (a.rows > kRowsPerCall) {
+    hipLaunchKernelGGL(k_sample_stats<NP>, dim3(a.tiles, a.rows), dim3(256), 0, st, a);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
+  hipLaunchKernelGGL(k_sample_rows<NP>, dim3(a.rows), dim3(kFinal), 0, st, a);
   if (const hipError_t e = hipGetLastError()) return e;
   hipLaunchKernelGGL(k_sample_weigh<NP>, dim3(a.parts, a.rows), dim3(256), 0, st, a);
   if (const hipError_t e = hipGetLastError()) return e;
@@ -816,10 +904,10 @@ extern "C" dbt_status dbt_sample(const dbt_sample_in *in, int32_t *token, float 
   a.u = in->u;
   a.rows = in->rows;
   a.V = in->vocab;
-  a.nb = in->n_branches;
+  a.Vp = round16(in->vocab);
   a.s = 62;
   for (int v = 1; v < in->vocab; v *= 2) --a.s;  // 2^s * vocab <= 2^62
-  if (a.s > 60) a.s = 60;
+  if (a.s > kMaxScale) a.s = kMaxScale;
   partition(a.rows, a.V, &a.tiles, &a.parts, &a.part);
   a.token = token;
   a.prob = prob;
