@@ -33,20 +33,22 @@ typedef unsigned long long u64;
 
 constexpr int kTile = 2048;         // tokens of one statistics tile
 constexpr int kMaxVocab = 1 << 20;
-constexpr int kRowsPerCall = 224;   // rows whose parameters travel with one launch
+constexpr int kParamSets = 96, kParamRows = 2048;  // different parameters, and rows, of one launch of the first kernel
 constexpr int kClasses = 256;       // weight classes: 0..253 by octave eighths, 254 everything lower, 255 weight zero
 constexpr int kLow = 254, kNone = 255;
 constexpr int kMaxScale = 46;       // s at most: the largest mixture value, within some 2^-52 of max m, has weight 2^s
 constexpr int kRankCap = 256;       // tokens that are ranked against each other
 constexpr int kFinal = 512;         // threads of the row kernels
 constexpr int kMaxParts = kMaxVocab / kTile;
+constexpr int kMaxPart = 4 * kTile;  // tokens of a part, at most
 
 struct RowParams {
   float t, top_p, min_p;
   int top_k;  // 0: no cut
 };
-struct ParamBlock {
-  RowParams r[kRowsPerCall];
+struct ParamBlock {  // (kernel arguments: below 4 KB)
+  RowParams set[kParamSets];
+  uint8_t of[kParamRows];  // each row's set
 };
 
 struct RowState {
@@ -125,6 +127,15 @@ __device__ __forceinline__ double log2_of(double r) {
   const double y = (double)__builtin_amdgcn_logf((float)m);
   const double d = fma(m, pow2(-y), -1.0);
   return (double)__builtin_amdgcn_frexp_exp(r) + y + d * fma(d, fma(d, 1.0 / 3, -0.5), 1.0) * kLog2eD;
+}
+
+// Logits i .. i + 3 of a row (rows start at any multiple of four bytes); past
+// `hi` its last one.
+typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ float4u load4(const float *z, int i, int hi) {
+  if (i + 4 <= hi) return *(const float4u *)(z + i);
+  const int e = hi - 1;
+  return float4u{z[min(i, e)], z[min(i + 1, e)], z[min(i + 2, e)], z[min(i + 3, e)]};
 }
 
 // scale_0 exp(z_0 - zmax_0) + ...: the same operations wherever it is evaluated
@@ -221,51 +232,44 @@ __device__ __forceinline__ void set_params(const Args &a, const RowParams &p, in
   r.listed = 0;
 }
 
-__global__ __launch_bounds__(kRowsPerCall) void k_sample_params(Args a, ParamBlock pb, int row0) {
-  if (row0 + (int)threadIdx.x < a.rows) set_params(a, pb.r[threadIdx.x], row0 + threadIdx.x);
-}
-
-// Statistics of one tile: each path's maximum and, with several paths, the sum
-// of exponentials; NaN for a tile that holds a NaN or +infinity.
+// Statistics of a tile by one wave: each path's maximum and, with several
+// paths, the sum of exponentials; NaN for a tile that holds a NaN or +infinity.
+// Each lane has its 32 values of a path in flight together.
 template <int NP>
-__device__ __forceinline__ void tile_stats(const Args &a, int tile, int row) {
-  __shared__ float red[16];
-  __shared__ double redd[16];
-  const int t = threadIdx.x;
-  float v[NP][8];
+__global__ __launch_bounds__(256) void k_sample_stats(Args a, ParamBlock pb, int row0) {
+  const int lane = threadIdx.x & 63, row = row0 + blockIdx.y;
+  const int tile = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (blockIdx.x == 0 && threadIdx.x == 0) set_params(a, pb.set[pb.of[blockIdx.y]], row);
+  if (tile >= a.tiles) return;
+  constexpr int N = kTile / 64;
 #pragma unroll
   for (int j = 0; j < NP; ++j) {
-    const float *z = path_row(a, j, row);
+    const float *z = path_row(a, j, row) + tile * kTile;
+    const int n = a.V - tile * kTile;
+    float v[N];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int i = tile * kTile + k * 256 + t;
-      v[j][k] = i < a.V ? z[i] : -INFINITY;
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < NP; ++j) {
+    for (int k = 0; k < N; ++k) v[k] = z[min(k * 64 + lane, n - 1)];
     float mx = -INFINITY;
     bool bad = false;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      mx = fmaxf(mx, v[j][k]);
-      bad |= !(v[j][k] < INFINITY);
+    for (int k = 0; k < N; ++k) {
+      mx = fmaxf(mx, v[k]);
+      bad |= !(v[k] < INFINITY);
     }
-    mx = block_max(mx, red);
+    mx = wave_max_dpp(mx);
     double sum = 0.0;
     if (NP > 1 && mx > -INFINITY) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) sum += pow2(((double)v[j][k] - (double)mx) * kLog2eD);
+      for (int k = 0; k < N; ++k) {
+        const double e = pow2(((double)v[k] - (double)mx) * kLog2eD);
+        sum += k * 64 + lane < n ? e : 0.0;  // (values past the row repeat its last)
+      }
     }
-    if (bad) sum = __longlong_as_double(0x7ff8000000000000ll);
-    sum = block_sum_d(sum, redd);
-    if (t == 0) a.w.stats[((size_t)row * a.tiles + tile) * 4 + j] = make_double2(mx, sum);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (__any(bad)) sum = __longlong_as_double(0x7ff8000000000000ll);
+    if (lane == 0) a.w.stats[((size_t)row * a.tiles + tile) * 4 + j] = make_double2(mx, sum);
   }
-}
-template <int NP> __global__ __launch_bounds__(256) void k_sample_stats(Args a) { tile_stats<NP>(a, blockIdx.x, blockIdx.y); }
-template <int NP> __global__ __launch_bounds__(256) void k_sample_stats_params(Args a, ParamBlock pb) {
-  if (blockIdx.x == 0 && threadIdx.x == 0) set_params(a, pb.r[blockIdx.y], blockIdx.y);
-  tile_stats<NP>(a, blockIdx.x, blockIdx.y);
 }
 
 // Row constants: every path's maximum and normaliser, and the largest mixture
@@ -321,17 +325,17 @@ __global__ __launch_bounds__(kFinal) void k_sample_rows(Args a) {
     if (t < a.tiles && ub >= lb) list[atomicAdd(&nlist, 1)] = t;  // (a maximum has no order)
     __syncthreads();
     double mx = 0.0;
-    for (int n = 0; n < nlist; ++n) {
-      float z[kTile / kFinal][NP];
+    // two tiles at a time, their loads in flight together (a last one twice)
+    constexpr int N = kTile / kFinal;
+    for (int n = 0; n < nlist; n += 2) {
+      float z[2 * N][NP];
 #pragma unroll
-      for (int k = 0; k < kTile / kFinal; ++k)
+      for (int k = 0; k < 2 * N; ++k)
 #pragma unroll
-        for (int j = 0; j < NP; ++j) {
-          const int i = list[n] * kTile + k * kFinal + t;
-          z[k][j] = i < a.V ? path_row(a, j, row)[i] : -INFINITY;
-        }
+        for (int j = 0; j < NP; ++j)
+          z[k][j] = path_row(a, j, row)[min(a.V - 1, list[min(n + k / N, nlist - 1)] * kTile + k % N * kFinal + t)];
 #pragma unroll
-      for (int k = 0; k < kTile / kFinal; ++k) mx = fmax(mx, mixture<NP>(rs, z[k]));
+      for (int k = 0; k < 2 * N; ++k) mx = fmax(mx, mixture<NP>(rs, z[k]));
     }
     mmax = block_max_d(mx, redd);
   }
@@ -360,30 +364,50 @@ __global__ __launch_bounds__(256) void k_sample_weigh(Args a) {
   __syncthreads();
   u64 kept = 0;  // no cut: kept mass; cut: mass of the low class
   unsigned low = 0;
-  for (int i0 = lo; i0 < hi; i0 += 1024) {
-    float z[4][NP];
+  // four neighbours a thread (their classes are one store), the next round's
+  // logits on their way while these are weighed
+  constexpr int Q = NP <= 2 ? 2 : 1;
+  float4u z[Q][NP], zn[Q][NP];
+  auto fetch = [&](int i0, float4u (&v)[Q][NP]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int j = 0; j < NP; ++j) z[k][j] = path_row(a, j, row)[min(i0 + k * 256 + t, hi - 1)];
+      for (int j = 0; j < NP; ++j) v[q][j] = load4(path_row(a, j, row), i0 + q * 1024 + t * 4, hi);
+  };
+  fetch(lo, zn);
+  for (int i0 = lo; i0 < hi; i0 += Q * 1024) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int i = i0 + k * 256 + t;
-      if (i >= hi) break;
-      const Weight w = weight<NP>(r, z[k], a.s);
-      if (!r.cut) {
-        if (w.w >= r.least) kept += w.w;
-        continue;
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int j = 0; j < NP; ++j) z[q][j] = zn[q][j];
+    if (i0 + Q * 1024 < hi) fetch(i0 + Q * 1024, zn);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int i = i0 + q * 1024 + t * 4;
+      if (i >= hi) continue;
+      uint32_t cls = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float ze[NP];
+#pragma unroll
+        for (int j = 0; j < NP; ++j) ze[j] = z[q][j][e];
+        const Weight w = weight<NP>(r, ze, a.s);
+        if (i + e >= hi) continue;
+        if (!r.cut) {
+          if (w.w >= r.least) kept += w.w;
+          continue;
+        }
+        const int c = weight_class(w.d, a.s);
+        cls |= (uint32_t)c << (8 * e);
+        if (c == kLow) {
+          kept += w.w;
+          ++low;
+        } else if (c < kLow) {
+          atomicAdd(&mass[c], w.w);
+          if (r.top_k > 0) atomicAdd(&count[c], 1u);
+        }
       }
-      const int c = weight_class(w.d, a.s);
-      a.w.cls[(size_t)row * a.Vp + i] = (uint8_t)c;
-      if (c == kLow) {
-        kept += w.w;
-        ++low;
-      } else if (c < kLow) {
-        atomicAdd(&mass[c], w.w);
-        if (r.top_k > 0) atomicAdd(&count[c], 1u);
-      }
+      if (r.cut) *(uint32_t *)(a.w.cls + (size_t)row * a.Vp + i) = cls;
     }
   }
   const int slot = r.cut ? kLow : 0;
@@ -484,7 +508,7 @@ __global__ __launch_bounds__(256) void k_sample_cut(Args a) {
 // Tokens of those classes, with their weights, in any order.
 template <int NP>
 __global__ __launch_bounds__(256) void k_sample_list(Args a) {
-  __shared__ int idx[4096];
+  __shared__ uint16_t idx[kMaxPart];
   __shared__ unsigned n_s, at_s;
   const int part = blockIdx.x, row = blockIdx.y, t = threadIdx.x;
   const RowState r = a.w.state[row];
@@ -492,31 +516,28 @@ __global__ __launch_bounds__(256) void k_sample_list(Args a) {
   const int kc = r.k_whole ? -1 : r.kc;
   const int lo = part * a.part, hi = min(a.V, lo + a.part);
   const uint8_t *cls = a.w.cls + (size_t)row * a.Vp;
-  for (int i0 = lo; i0 < hi; i0 += 4096) {
-    if (t == 0) n_s = 0;
-    __syncthreads();
-    const int i = i0 + t * 16;
-    if (i < hi) {
-      const u32x4 v = *(const u32x4 *)(cls + i);
+  if (t == 0) n_s = 0;
+  __syncthreads();
+  for (int i = lo + t * 16; i < hi; i += 256 * 16) {
+    const u32x4 v = *(const u32x4 *)(cls + i);
 #pragma unroll
-      for (int b = 0; b < 16; ++b) {
-        const int c = (v[b >> 2] >> (8 * (b & 3))) & 0xff;
-        if (((c >= r.pl && c <= r.ph) || c == kc || c == r.lc) && c <= kLow && i + b < hi) idx[atomicAdd(&n_s, 1u)] = i + b;
-      }
+    for (int b = 0; b < 16; ++b) {
+      const int c = (v[b >> 2] >> (8 * (b & 3))) & 0xff;
+      if (((c >= r.pl && c <= r.ph) || c == kc || c == r.lc) && c <= kLow && i + b < hi) idx[atomicAdd(&n_s, 1u)] = (uint16_t)(i + b - lo);
     }
-    __syncthreads();
-    const unsigned n = n_s;
-    if (t == 0 && n) at_s = atomicAdd(&a.w.state[row].listed, n);
-    __syncthreads();
-    for (unsigned k = t; k < n; k += 256) {
-      float z[NP];
+  }
+  __syncthreads();
+  const unsigned n = n_s;
+  if (t == 0 && n) at_s = atomicAdd(&a.w.state[row].listed, n);
+  __syncthreads();
+  for (unsigned k = t; k < n; k += 256) {
+    const int i = lo + idx[k];
+    float z[NP];
 #pragma unroll
-      for (int j = 0; j < NP; ++j) z[j] = path_row(a, j, row)[idx[k]];
-      const size_t o = (size_t)row * a.V + at_s + k;
-      a.w.lw[o] = weight<NP>(r, z, a.s).w;
-      a.w.li[o] = idx[k];
-    }
-    __syncthreads();
+    for (int j = 0; j < NP; ++j) z[j] = path_row(a, j, row)[i];
+    const size_t o = (size_t)row * a.V + at_s + k;
+    a.w.lw[o] = weight<NP>(r, z, a.s).w;
+    a.w.li[o] = i;
   }
 }
 
@@ -525,7 +546,7 @@ struct FinalShared {
   unsigned count[256];
   u64 rw[kRankCap];
   int ri[kRankCap];
-  u64 pmass[kMaxParts];
+  u64 pmass[kMaxParts], runs[kMaxPart / kTile * (kFinal / 64)];
   u64 red[kFinal / 64];
   u64 cut_w, sum, need;
   int cut_i, n, bin, token;
@@ -566,20 +587,48 @@ __device__ __forceinline__ void pick_bin(FinalShared &sh, u64 need, bool by_mass
   }
 }
 
+// A row's listed tokens as its workgroup goes over them: a list that fits sits
+// in registers, loaded once with every load in flight; others are read again.
+struct Listed {
+  static constexpr int N = 8;
+  const u64 *lw;
+  const int *li;
+  int n;
+  u64 w[N];
+  int i[N];
+  __device__ __forceinline__ void load() {
+    if (n > N * kFinal) return;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int e = k * kFinal + (int)threadIdx.x;
+      w[k] = e < n ? lw[e] : 0;  // (weight zero: in no range)
+      i[k] = e < n ? li[e] : 0;
+    }
+  }
+  template <typename F> __device__ __forceinline__ void each(F f) const {
+    if (n <= N * kFinal) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) f(w[k], i[k]);
+    } else {
+      for (int e = threadIdx.x; e < n; e += kFinal) f(lw[e], li[e]);
+    }
+  }
+};
+
 // Where the order by (weight falling, index) is cut among the listed weights of
 // [lo, hi), `inside` of them, after `need` tokens (by_mass: after the shortest run
 // whose mass reaches need; the range holds as much): the last token that stays
 // in sh.cut_w, sh.cut_i, the mass that stays of the range in sh.sum.  Ranges of
 // more than kRankCap tokens are narrowed 256-fold by histograms of the weight and, once all
 // weights are equal, of the index.
-__device__ void cut_range(FinalShared &sh, const u64 *lw, const int *li, int n, int V, u64 lo, u64 hi, u64 need, bool by_mass) {
+__device__ __forceinline__ void cut_range(FinalShared &sh, const Listed &list, int V, u64 lo, u64 hi, u64 need, bool by_mass) {
   const int t = threadIdx.x;
   u64 above = 0;  // mass that stays above the narrowed range
   int ilo = 0, ihi = V;
   unsigned inside = 0;
   {
     unsigned mine = 0;
-    for (int i = t; i < n; i += kFinal) mine += lw[i] >= lo && lw[i] < hi;
+    list.each([&](u64 w, int) { mine += w >= lo && w < hi; });
     const u64 w = wave_sum64(mine);
     __syncthreads();
     if ((t & 63) == 0) sh.red[t >> 6] = w;
@@ -600,14 +649,12 @@ __device__ void cut_range(FinalShared &sh, const u64 *lw, const int *li, int n, 
       sh.count[t] = 0;
     }
     __syncthreads();
-    for (int i = t; i < n; i += kFinal) {
-      const u64 w = lw[i];
-      const int ix = li[i];
-      if (w < lo || w >= hi || ix < ilo || ix >= ihi) continue;
+    list.each([&](u64 w, int ix) {
+      if (w < lo || w >= hi || ix < ilo || ix >= ihi) return;
       const int b = by_index ? (ix - ilo) >> shift : (int)((w - lo) >> shift);
       atomicAdd(&sh.mass[b], w);
       atomicAdd(&sh.count[b], 1u);
-    }
+    });
     __syncthreads();
     if (t < 64) pick_bin(sh, need, by_mass, !by_index);
     __syncthreads();
@@ -625,16 +672,14 @@ __device__ void cut_range(FinalShared &sh, const u64 *lw, const int *li, int n, 
   __syncthreads();
   if (t == 0) sh.n = 0;
   __syncthreads();
-  for (int i = t; i < n; i += kFinal) {
-    const u64 w = lw[i];
-    const int ix = li[i];
-    if (w < lo || w >= hi || ix < ilo || ix >= ihi) continue;
+  list.each([&](u64 w, int ix) {
+    if (w < lo || w >= hi || ix < ilo || ix >= ihi) return;
     const int k = atomicAdd(&sh.n, 1);  // (any order: ranks come from weight and index)
     if (k < kRankCap) {
       sh.rw[k] = w;
       sh.ri[k] = ix;
     }
-  }
+  });
   if (t == 0) {
     sh.cut_w = lo;
     sh.cut_i = V;
@@ -678,12 +723,12 @@ __global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
     }
     return;
   }
-  const u64 *lw = a.w.lw + (size_t)row * a.V;
-  const int *li = a.w.li + (size_t)row * a.V;
   const u64 *tm = a.w.tmass + (size_t)row * a.parts * kClasses;
   // stays: W > cut_w, or W == cut_w and the index at most cut_i
   u64 cut_w = 1;
   int cut_i = a.V;
+  Listed list{a.w.lw + (size_t)row * a.V, a.w.li + (size_t)row * a.V, r.cut ? (int)r.listed : 0};
+  list.load();
   if (r.cut) {
     const u64 *upto = a.w.upto + (size_t)row * kClasses;
     u64 total = upto[kLow], lo, hi;
@@ -693,7 +738,7 @@ __global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
         total = upto[r.kc];
         cut_w = lo;
       } else {
-        cut_range(sh, lw, li, r.listed, a.V, lo, hi, r.k_need, false);
+        cut_range(sh, list, a.V, lo, hi, r.k_need, false);
         total = r.k_mass + sh.sum;
         cut_w = sh.cut_w;
         cut_i = sh.cut_i;
@@ -706,7 +751,7 @@ __global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
       while (c < r.ph && upto[c] < need) ++c;
       class_range(c, a.s, lo, hi);
       __syncthreads();
-      cut_range(sh, lw, li, r.listed, a.V, lo, hi, need - (c ? upto[c - 1] : 0), true);
+      cut_range(sh, list, a.V, lo, hi, need - (c ? upto[c - 1] : 0), true);
       cut_w = sh.cut_w;
       cut_i = sh.cut_i;
     }
@@ -736,10 +781,9 @@ __global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
     }
     __syncthreads();
     if (!whole)
-      for (int i = t; i < (int)r.listed; i += kFinal) {
-        const u64 w = lw[i];
-        if (w < hi && (w > cut_w || (w == cut_w && li[i] <= cut_i))) atomicAdd(&sh.pmass[li[i] / a.part], w);
-      }
+      list.each([&](u64 w, int ix) {
+        if (w < hi && (w > cut_w || (w == cut_w && ix <= cut_i))) atomicAdd(&sh.pmass[ix / a.part], w);
+      });
   } else {
     for (int p = t; p < a.parts; p += kFinal) sh.pmass[p] = tm[(size_t)p * kClasses];
   }
@@ -769,37 +813,58 @@ __global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
     sh.sum = incl - m;
   }
   __syncthreads();
-  // the token: each wave sums a run of the part, the one that holds the target scans it
+  // the token: sums of every 256 neighbours by the waves, then the wave that
+  // holds the target weighs its 256 again and finds the token
+  constexpr int PER = kTile / kFinal, RUN = PER * 64;
   const int p0 = sh.bin * a.part, n = min(a.V, p0 + a.part) - p0;
   before = sh.sum;
-  auto get = [&](int i) __attribute__((always_inline)) {
-    float z[NP];
+  auto run = [&](int s0, u64 (&w)[PER]) __attribute__((always_inline)) {  // weights s0 + 64 k + lane that stay
+    float z[PER][NP];
 #pragma unroll
-    for (int j = 0; j < NP; ++j) z[j] = path_row(a, j, row)[p0 + min(i, n - 1)];
-    const u64 w = weight<NP>(r, z, a.s).w;
-    return i < n && (w > cut_w || (w == cut_w && p0 + i <= cut_i)) ? w : 0;
-  };
-  const int seg = ((n + NW - 1) / NW + 63) / 64 * 64, s0 = wave * seg, s1 = min(n, s0 + seg);
-  u64 sum = 0;
-#pragma unroll 4
-  for (int i = s0; i < s1; i += 64) sum += get(i + lane);
-  sum = wave_sum64(sum);
-  if (lane == 0) sh.red[wave] = sum;
-  __syncthreads();
-  for (int k = 0; k < wave; ++k) before += sh.red[k];
-  if (before <= target && target < before + sum)
-    for (int i = s0; i < s1; i += 64) {
-      const u64 w = get(i + lane), upto_i = before + wave_scan64(w);
-      const u64 hit = __ballot(upto_i > target);
-      if (hit) {
-        if (lane == __ffsll(hit) - 1) {
-          a.token[row] = p0 + i + lane;
-          if (a.prob) a.prob[row] = r.greedy ? 1.f : (float)((double)w / (double)total);
-        }
-        break;
-      }
-      before = __shfl(upto_i, 63, 64);
+    for (int k = 0; k < PER; ++k)
+#pragma unroll
+      for (int j = 0; j < NP; ++j) z[k][j] = path_row(a, j, row)[p0 + min(s0 + k * 64 + lane, n - 1)];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int i = s0 + k * 64 + lane;
+      const u64 x = weight<NP>(r, z[k], a.s).w;
+      w[k] = i < n && (x > cut_w || (x == cut_w && p0 + i <= cut_i)) ? x : 0;
     }
+  };
+#pragma unroll 1
+  for (int c = 0; c < kMaxPart / kTile; ++c) {
+    u64 w[PER], sum = 0;
+    if (c * kTile + wave * RUN < n) {
+      run(c * kTile + wave * RUN, w);
+#pragma unroll
+      for (int k = 0; k < PER; ++k) sum += w[k];
+      sum = wave_sum64(sum);
+    }
+    if (lane == 0) sh.runs[c * NW + wave] = sum;
+  }
+  __syncthreads();
+  static_assert(kMaxPart / kTile * NW <= 64, "one run per lane");
+  u64 mine = lane < kMaxPart / kTile * NW ? sh.runs[lane] : 0, runs = before + wave_scan64(mine);
+  const u64 at = __ballot(target < runs);
+  const int pick = __ffsll(at) - 1;  // (every wave agrees)
+  if (pick >= 0 && pick % NW == wave) {
+    before = __shfl(runs - mine, pick, 64);
+    const int s0 = pick / NW * kTile + wave * RUN;
+    u64 w[PER];
+    run(s0, w);
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const u64 upto_i = before + wave_scan64(w[k]), end = __shfl(upto_i, 63, 64);
+      if (before <= target && target < end) {
+        const u64 hit = __ballot(upto_i > target);
+        if (lane == __ffsll(hit) - 1) {
+          a.token[row] = p0 + s0 + k * 64 + lane;
+          if (a.prob) a.prob[row] = r.greedy ? 1.f : (float)((double)w[k] / (double)total);
+        }
+      }
+      before = end;
+    }
+  }
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -809,7 +874,7 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 void partition(int rows, int vocab, int *tiles, int *parts, int *part) {
   *tiles = (vocab + kTile - 1) / kTile;
   int f = 1;
-  while (f < 4 && (long long)rows * ((*tiles + f) / (f + 1)) >= 1024) ++f;
+  while (f < kMaxPart / kTile && (long long)rows * ((*tiles + f) / (f + 1)) >= 1024) ++f;
   *part = f * kTile;
   *parts = (vocab + *part - 1) / *part;
 }
@@ -842,20 +907,25 @@ size_t layout(int rows, int vocab, char *base, Work *w) {
 dbt_status fail(dbt_status s, const char *msg) { return set_error(s, msg); }
 
 template <int NP> hipError_t launch(const Args &a, const dbt_sampling *p, bool cuts, hipStream_t st) {
-  for (int r0 = 0; r0 < a.rows; r0 += kRowsPerCall) {
+  for (int r0 = 0; r0 < a.rows;) {
+    // rows while their parameters fit (the requests of a batch, or the nodes of
+    // a request's tree, share them)
     ParamBlock pb;
-    const int n = a.rows - r0 < kRowsPerCall ? a.rows - r0 : kRowsPerCall;
-    for (int i = 0; i < n; ++i)
-      pb.r[i] = RowParams{p[r0 + i].temperature, p[r0 + i].top_p, p[r0 + i].min_p, p[r0 + i].top_k};
-    if (a.rows <= kRowsPerCall)  // (a launch fewer)
-      hipLaunchKernelGGL(k_sample_stats_params<NP>, dim3(a.tiles, n), dim3(256), 0, st, a, pb);
-    else
-      hipLaunchKernelGGL(k_sample_params, dim3(1), dim3(kRowsPerCall), 0, st, a, pb, r0);
+    int n = 0, sets = 0, last = -1;
+    for (; r0 + n < a.rows && n < kParamRows; ++n) {
+      const dbt_sampling &q = p[r0 + n];
+      auto same = [&](int k) {
+        return pb.set[k].t == q.temperature && pb.set[k].top_p == q.top_p && pb.set[k].min_p == q.min_p && pb.set[k].top_k == q.top_k;
+      };
+      int k = last >= 0 && same(last) ? last : 0;
+      while (k < sets && !same(k)) ++k;
+      if (k == kParamSets) break;
+      if (k == sets) pb.set[sets++] = RowParams{q.temperature, q.top_p, q.min_p, q.top_k};
+      pb.of[n] = (uint8_t)(last = k);
+    }
+    hipLaunchKernelGGL(k_sample_stats<NP>, dim3((a.tiles + 3) / 4, n), dim3(256), 0, st, a, pb, r0);
     if (const hipError_t e = hipGetLastError()) return e;
-  }
-  if (a.rows > kRowsPerCall) {
-    hipLaunchKernelGGL(k_sample_stats<NP>, dim3(a.tiles, a.rows), dim3(256), 0, st, a);
-    if (const hipError_t e = hipGetLastError()) return e;
+    r0 += n;
   }
   hipLaunchKernelGGL(k_sample_rows<NP>, dim3(a.rows), dim3(kFinal), 0, st, a);
   if (const hipError_t e = hipGetLastError()) return e;
