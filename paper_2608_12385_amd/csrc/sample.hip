@@ -37,7 +37,7 @@ constexpr int kParamSets = 96, kParamRows = 2048;  // different parameters, and 
 constexpr int kClasses = 256;       // weight classes: 0..253 by octave eighths, 254 everything lower, 255 weight zero
 constexpr int kLow = 254, kNone = 255;
 constexpr int kMaxScale = 46;       // s at most: the largest mixture value, within some 2^-52 of max m, has weight 2^s
-constexpr int kRankCap = 256;       // tokens that are ranked against each other
+constexpr int kRankCap = 64;        // tokens that are ranked against each other
 constexpr int kFinal = 512;         // threads of the row kernels
 constexpr int kMaxParts = kMaxVocab / kTile;
 constexpr int kMaxPart = 4 * kTile;  // tokens of a part, at most
@@ -831,7 +831,7 @@ __global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
       w[k] = i < n && (x > cut_w || (x == cut_w && p0 + i <= cut_i)) ? x : 0;
     }
   };
-#pragma unroll 1
+#pragma unroll 2
   for (int c = 0; c < kMaxPart / kTile; ++c) {
     u64 w[PER], sum = 0;
     if (c * kTile + wave * RUN < n) {
@@ -874,7 +874,7 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 void partition(int rows, int vocab, int *tiles, int *parts, int *part) {
   *tiles = (vocab + kTile - 1) / kTile;
   int f = 1;
-  while (f < kMaxPart / kTile && (long long)rows * ((*tiles + f) / (f + 1)) >= 1024) ++f;
+  while (f < kMaxPart / kTile && (long long)rows * ((*tiles + f) / (f + 1)) >= 2048) ++f;
   *part = f * kTile;
   *parts = (vocab + *part - 1) / *part;
 }
