@@ -64,7 +64,8 @@ struct RowState {
   int kc, k_need;   // class in which top-k cuts and how many of it stay (kc = -1: nothing is cut)
   int k_whole;      // that class stays whole
   int pl, ph;       // classes in which top-p can cut (pl > ph: none)
-  int lc;           // class of `least` (-1: no such cut)
+  int lc;           // class of `least` if min-p can be the lowest cut (else -1)
+  int l0, l1;       // those classes lie in l0 .. l1 (l0 > l1: none)
   unsigned listed;
 };
 
@@ -95,6 +96,14 @@ __device__ __forceinline__ const float *path_row(const Args &a, int j, int row) 
 
 constexpr double kLog2eD = 1.4426950408889634074;
 
+// a b + c with c in scalar registers (the compiler copies such a constant into
+// the result's registers first, one more instruction each).
+__device__ __forceinline__ double fma_s(double a, double b, double c) {
+  double r;
+  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
+  return r;
+}
+
 // 2^t for t <= 0 (and small t above), within 1e-14: t = n + f, |f| <= 1/2, and the
 // Taylor series of 2^f = e^(f ln 2) to the eleventh power (its remainder is below
 // (ln 2 / 2)^12 / 12! = 6.3e-15).  Sixteen instructions; the library's exp takes
@@ -105,17 +114,16 @@ __device__ __forceinline__ double pow2(double t) {
                    c8 = c7 * L / 8, c9 = c8 * L / 9, c10 = c9 * L / 10, c11 = c10 * L / 11;
   t = fmax(t, -1200.0);
   const double n = rint(t), f = t - n;
-  double p = c11;
-  p = fma(p, f, c10);
-  p = fma(p, f, c9);
-  p = fma(p, f, c8);
-  p = fma(p, f, c7);
-  p = fma(p, f, c6);
-  p = fma(p, f, c5);
-  p = fma(p, f, c4);
-  p = fma(p, f, c3);
-  p = fma(p, f, c2);
-  p = fma(p, f, c1);
+  double p = fma(f, c11, c10);
+  p = fma_s(p, f, c9);
+  p = fma_s(p, f, c8);
+  p = fma_s(p, f, c7);
+  p = fma_s(p, f, c6);
+  p = fma_s(p, f, c5);
+  p = fma_s(p, f, c4);
+  p = fma_s(p, f, c3);
+  p = fma_s(p, f, c2);
+  p = fma_s(p, f, c1);
   p = fma(p, f, 1.0);
   return __builtin_amdgcn_ldexp(p, (int)n);
 }
@@ -129,13 +137,15 @@ __device__ __forceinline__ double log2_of(double r) {
   return (double)__builtin_amdgcn_frexp_exp(r) + y + d * fma(d, fma(d, 1.0 / 3, -0.5), 1.0) * kLog2eD;
 }
 
-// Logits i .. i + 3 of a row (rows start at any multiple of four bytes); past
-// `hi` its last one.
+// Logits i .. i + 3 of a row (rows start at any multiple of four bytes); from
+// `hi` on those of tokens without weight.
 typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ float4u load4(const float *z, int i, int hi) {
   if (i + 4 <= hi) return *(const float4u *)(z + i);
-  const int e = hi - 1;
-  return float4u{z[min(i, e)], z[min(i + 1, e)], z[min(i + 2, e)], z[min(i + 3, e)]};
+  float4u v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = i + e < hi ? z[i + e] : -INFINITY;
+  return v;
 }
 
 // scale_0 exp(z_0 - zmax_0) + ...: the same operations wherever it is evaluated
@@ -385,29 +395,32 @@ __global__ __launch_bounds__(256) void k_sample_weigh(Args a) {
     for (int q = 0; q < Q; ++q) {
       const int i = i0 + q * 1024 + t * 4;
       if (i >= hi) continue;
-      uint32_t cls = 0;
+      Weight w[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float ze[NP];
 #pragma unroll
         for (int j = 0; j < NP; ++j) ze[j] = z[q][j][e];
-        const Weight w = weight<NP>(r, ze, a.s);
-        if (i + e >= hi) continue;
-        if (!r.cut) {
-          if (w.w >= r.least) kept += w.w;
-          continue;
-        }
-        const int c = weight_class(w.d, a.s);
+        w[e] = weight<NP>(r, ze, a.s);
+      }
+      if (!r.cut) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) kept += w[e].w >= r.least ? w[e].w : 0;
+        continue;
+      }
+      uint32_t cls = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = weight_class(w[e].d, a.s);
         cls |= (uint32_t)c << (8 * e);
-        if (c == kLow) {
-          kept += w.w;
-          ++low;
-        } else if (c < kLow) {
-          atomicAdd(&mass[c], w.w);
+        kept += c == kLow ? w[e].w : 0;
+        low += c == kLow;
+        if (c < kLow) {
+          atomicAdd(&mass[c], w[e].w);
           if (r.top_k > 0) atomicAdd(&count[c], 1u);
         }
       }
-      if (r.cut) *(uint32_t *)(a.w.cls + (size_t)row * a.Vp + i) = cls;
+      *(uint32_t *)(a.w.cls + (size_t)row * a.Vp + i) = cls;
     }
   }
   const int slot = r.cut ? kLow : 0;
@@ -501,18 +514,34 @@ __global__ __launch_bounds__(256) void k_sample_cut(Args a) {
     r.k_mass = kc > 0 ? ms[kc - 1] : 0;
     r.pl = top_p < 1.f ? pl_s : 0;
     r.ph = top_p < 1.f ? ph_s : -1;
-    r.lc = r.least > 1 ? weight_class((double)r.least, a.s) : -1;
+    int l0 = kClasses, l1 = -1;
+    if (kc >= 0 && !whole) l0 = l1 = kc;
+    if (top_p < 1.f) {
+      l0 = min(l0, pl_s);
+      l1 = max(l1, ph_s);
+    }
+    int lc = r.least > 1 ? weight_class((double)r.least, a.s) : -1;
+    if (lc > (l1 >= 0 ? l1 : kc >= 0 ? kc : kLow)) lc = -1;  // the other cuts have removed what it would
+    if (lc >= 0) {
+      l1 = lc < l0 ? lc : l1;  // above every other cut: those do not matter
+      l0 = min(l0, lc);
+    }
+    r.lc = lc;
+    r.l0 = l0;
+    r.l1 = l1;
   }
 }
 
-// Tokens of those classes, with their weights, in any order.
+// Tokens of those classes, with their weights, in any order.  (One test a token
+// for nearly all of them; the exact one for those that pass it: between the
+// classes of top-p and of top-k may lie almost top_k tokens.)
 template <int NP>
 __global__ __launch_bounds__(256) void k_sample_list(Args a) {
   __shared__ uint16_t idx[kMaxPart];
   __shared__ unsigned n_s, at_s;
   const int part = blockIdx.x, row = blockIdx.y, t = threadIdx.x;
   const RowState r = a.w.state[row];
-  if (!r.valid || !r.cut) return;
+  if (!r.valid || !r.cut || r.l0 > r.l1) return;
   const int kc = r.k_whole ? -1 : r.kc;
   const int lo = part * a.part, hi = min(a.V, lo + a.part);
   const uint8_t *cls = a.w.cls + (size_t)row * a.Vp;
@@ -523,7 +552,8 @@ __global__ __launch_bounds__(256) void k_sample_list(Args a) {
 #pragma unroll
     for (int b = 0; b < 16; ++b) {
       const int c = (v[b >> 2] >> (8 * (b & 3))) & 0xff;
-      if (((c >= r.pl && c <= r.ph) || c == kc || c == r.lc) && c <= kLow && i + b < hi) idx[atomicAdd(&n_s, 1u)] = (uint16_t)(i + b - lo);
+      if ((unsigned)(c - r.l0) <= (unsigned)(r.l1 - r.l0) && ((c >= r.pl && c <= r.ph) || c == kc || c == r.lc) && i + b < hi)
+        idx[atomicAdd(&n_s, 1u)] = (uint16_t)(i + b - lo);
     }
   }
   __syncthreads();
