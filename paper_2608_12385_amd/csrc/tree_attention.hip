@@ -129,313 +129,313 @@ k_tree_attn_bf16(TreeAttn a) {
   const int place_w = schedule_place(blockIdx.x, gridDim.x), w = place_w / a.blocks, blk = place_w % a.blocks;
   const int end = min(a.s.first[a.s.n], (w + 1) * a.s.per);
   for (int at = w * a.s.per; at < end;) {
-  const Piece pc = piece_at(a, at, end);
-  at += a.s.whole ? 1 : pc.st1 - pc.st0;
-  const int i = pc.i, g = pc.g;
-  const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
-  const int rows = n * a.np * G, row0 = blk * (RW * RT * 16);
-  if (row0 >= rows) continue;
-  const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
-  const int *ptab = a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps;
-  const int pages0 = pc.st0 * 8, pages1 = min((len + 15) >> 4, pc.st1 * 8);  // the piece's pages
-  int pb = pages0, npg = min(pages1 - pb, kWindow * 8);  // the window's first page, its pages
-  __syncthreads();  // (the last piece's readers)
-  for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
-  if (wave == 0) line_s[lane] = node_line(a.parents + first, n);
-  __syncthreads();
-
-  // K row j of a page holds its 16-byte chunk c at c ^ kswz(j): the score operand
-  // reads rows {0..3, 8..11} (or {4..7, 12..15}) of both pages at one chunk
-  // without bank conflicts.  V rows (one dimension, 32 bytes) need no swizzle.
-  auto kswz = [](int row) { return ((row & 3) | ((row >> 3) << 2)) << 1; };
-  const uint16_t *kbase = (const uint16_t *)a.kv.k, *vbase = (const uint16_t *)a.kv.v;
-  // A stage is 64 loads of 1 KB, four of K and four of V a page: each wave takes
-  // 64 / NW.  Pages past the split's last re-read it (never used unmasked).
-  auto dma = [&](int st, uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
-#pragma unroll
-    for (int p = 0; p < SP / NW; ++p) {
-      const int page = wave * (SP / NW) + p;
-      const int phys = __builtin_amdgcn_readfirstlane(pid_s[min(st * SP + page, npg - 1)]);
-      const size_t at = ((size_t)phys * n_kv + g) * PB;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int row = 4 * j + (lane >> 4);
-        __builtin_amdgcn_global_load_lds((const void *)(kbase + at + row * DH + ((lane & 15) ^ kswz(row)) * 8),
-                                         (lds_void *)(kb + page * PB + 4 * j * DH), 16, 0, 0);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        __builtin_amdgcn_global_load_lds((const void *)(vbase + at + 32 * j * 16 + lane * 8),
-                                         (lds_void *)(vb + page * PB + 32 * j * 16), 16, 0, 0);
-    }
-  };
-
-  dma(0, kl0, vl0);  // (the queries' loads run beside it)
-
-  const int wrow = row0 + rw * RT * 16;  // the wave's first row
-  u32x4 qf[RT][4];
-  uint64_t line[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int rho = wrow + rt * 16 + r;
-    const bool live = rho < rows;
-    line[rt] = live ? line_s[rho / (G * a.np)] : 0;
-    const QT *qp = (const QT *)a.Q + place(live ? rho : 0) * DH + gq * 8;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      if constexpr (sizeof(QT) == 2) {
-        qf[rt][s] = *(const u32x4 *)(qp + s * 32);
-      } else {  // the projections' queries, rounded once to the cache's type as in a step
-        const float4 x = *(const float4 *)(qp + s * 32), y = *(const float4 *)(qp + s * 32 + 4);
-        qf[rt][s] = u32x4{pack2(x.x, x.y), pack2(x.z, x.w), pack2(y.x, y.y), pack2(y.z, y.w)};
-      }
-      if (!live) qf[rt][s] = u32x4{0, 0, 0, 0};
-    }
-  }
-
-  float m_run[RT];
-  floatx4 acc[RT][8], acc_l[RT];  // acc_l: the sums of the rounded probabilities, by one more value multiply with V = 1
-  const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    m_run[rt] = kNoScore;
-    acc_l[rt] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < 8; ++c) acc[rt][c] = floatx4{0.f, 0.f, 0.f, 0.f};
-  }
-  const int kpage = r >> 3, kpos = 8 * ((r >> 2) & 1) + (r & 3);
-  const int vpage = gq >> 1, vpos = 8 * (gq & 1);
-  const bool active = wrow < rows;
-  bool odd = false;  // some node's value is not finite
-
-  auto pair = [&](int pg0, const uint16_t *kb, const uint16_t *vb, auto masked) __attribute__((always_inline)) {
-    constexpr bool MASKED = decltype(masked)::value;
-    u32x4 ka[4], kc[4], vf[8];
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      ka[s] = *(const u32x4 *)&kb[(kpage * 16 + kpos) * DH + ((s * 4 + gq) ^ kswz(kpos)) * 8];
-      kc[s] = *(const u32x4 *)&kb[(kpage * 16 + kpos + 4) * DH + ((s * 4 + gq) ^ kswz(kpos + 4)) * 8];
-    }
-    floatx4 sc[RT][2];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      sc[rt][0] = sc[rt][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        sc[rt][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka[s]),
-                                                            __builtin_bit_cast(bf16x8, qf[rt][s]), sc[rt][0], 0, 0, 0);
-        sc[rt][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kc[s]),
-                                                            __builtin_bit_cast(bf16x8, qf[rt][s]), sc[rt][1], 0, 0, 0);
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < 8; ++c) vf[c] = *(const u32x4 *)&vb[(vpage * DH + c * 16 + r) * 16 + vpos];
-    const int kp0 = (pb + pg0 + vpage) * 16 + vpos;  // position of this lane's first score
-    const bool page_ok = pg0 + vpage < npg;
-    if (MASKED) {
-      // slots past the sequence may hold anything; a node's values that are not
-      // finite would reach the rows that do not see it as 0 * infinity, so
-      // they are taken out here and added at the end
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        vf[c] = mask8(vf[c], kp0, page_ok ? len : kp0);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t x = vf[c][w];
-          const bool lo = (x & 0x7f80u) == 0x7f80u && kp0 + 2 * w >= base;
-          const bool hi = (x & 0x7f800000u) == 0x7f800000u && kp0 + 2 * w + 1 >= base;
-          odd |= lo | hi;
-          vf[c][w] = x & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
-        }
-      }
-    }
-    // (the row tiles' steps side by side: one tile alone leaves the units waiting
-    // for its chain of maximum, exponentials and conversion)
-    float s[RT][8], m_new[RT];
-    bool grow = false;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[rt][e] = sc[rt][0][e];
-        s[rt][4 + e] = sc[rt][1][e];
-      }
-      if (MASKED) {  // the row's eight positions: before `base`, or on its line
-        const int rel = kp0 - base;
-        const uint32_t seen = !page_ok || rel >= 64 ? 0u
-                              : rel >= 0            ? (uint32_t)(line[rt] >> rel) & 0xff
-                              : rel > -8            ? (uint32_t)((line[rt] << -rel) | ((1u << -rel) - 1)) & 0xff
-                                                    : 0xffu;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (!((seen >> e) & 1)) s[rt][e] = -INFINITY;
-      }
-      float mt = s[rt][0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) mt = fmaxf(mt, s[rt][e]);
-      // lazy rescaling: a row's base moves only when the pair's maximum exceeds it
-      // by more than kLazyMargin, so exponentials stay <= 2^kLazyMargin
-      const float mt_s = rows4_max(mt) * scale;
-      const bool up = mt_s > m_run[rt] + kLazyMargin;
-      m_new[rt] = up ? mt_s : m_run[rt];
-      grow |= up;
-    }
-    if (__any(grow)) {  // (a factor of exactly 1 where the base stays)
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const float corr = __builtin_amdgcn_exp2f(m_run[rt] - m_new[rt]);
-        acc_l[rt] = acc_l[rt] * corr;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) acc[rt][c] = acc[rt][c] * corr;
-        m_run[rt] = m_new[rt];
-      }
-    }
-    u32x4 pf[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][e], scale, -m_new[rt]));
-      // (probabilities are rounded to bf16 for the matrix unit; their sum is of the rounded ones)
-      pf[rt] = u32x4{pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7])};
-    }
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      acc_l[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones),
-                                                          __builtin_bit_cast(bf16x8, pf[rt]), acc_l[rt], 0, 0, 0);
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        acc[rt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[c]),
-                                                             __builtin_bit_cast(bf16x8, pf[rt]), acc[rt][c], 0, 0, 0);
-    }
-  };
-  auto stage = [&](int st, const uint16_t *kb, const uint16_t *vb, auto masked) __attribute__((always_inline)) {
-    if (!active) return;
-#pragma unroll 1
-    for (int j = 0; j < PP; ++j) {
-      const int pi = kw * PP + j, pg0 = st * SP + 2 * pi;
-      if (decltype(masked)::value && pg0 >= npg) break;
-      pair(pg0, kb + 2 * pi * PB, vb + 2 * pi * PB, masked);
-    }
-  };
-  // The barrier in front of a stage waits for its loads and for the readers of
-  // the other set, which the next stage's loads then fill.  Stages of which
-  // every row sees every key first, in pairs so that each set is known; then
-  // the last ones, those from the page of position `base` on.
-  for (;;) {
-    const int nst = (npg + SP - 1) / SP, nfull = max(0, min(npg, (base >> 4) - pb)) / SP;
-    for (int st = 0; st < nfull; st += 2) {
-      __syncthreads();
-      if (st + 1 < nst) dma(st + 1, kl1, vl1);
-      __builtin_amdgcn_sched_barrier(0);
-      stage(st, kl0, vl0, std::false_type{});
-      if (st + 1 < nfull) {
-        __syncthreads();
-        if (st + 2 < nst) dma(st + 2, kl0, vl0);
-        __builtin_amdgcn_sched_barrier(0);
-        stage(st + 1, kl1, vl1, std::false_type{});
-      }
-    }
-#pragma unroll 1
-    for (int st = nfull; st < nst; ++st) {
-      __syncthreads();
-      const bool set1 = st & 1;
-      if (st + 1 < nst) dma(st + 1, set1 ? kl0 : kl1, set1 ? vl0 : vl1);
-      stage(st, set1 ? kl1 : kl0, set1 ? vl1 : vl0, std::true_type{});
-    }
-    pb += kWindow * 8;
-    if (pb >= pages1) break;
-    npg = min(pages1 - pb, kWindow * 8);
-    __syncthreads();
+    const Piece pc = piece_at(a, at, end);
+    at += a.s.whole ? 1 : pc.st1 - pc.st0;
+    const int i = pc.i, g = pc.g;
+    const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
+    const int rows = n * a.np * G, row0 = blk * (RW * RT * 16);
+    if (row0 >= rows) continue;
+    const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
+    const int *ptab = a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps;
+    const int pages0 = pc.st0 * 8, pages1 = min((len + 15) >> 4, pc.st1 * 8);  // the piece's pages
+    int pb = pages0, npg = min(pages1 - pb, kWindow * 8);  // the window's first page, its pages
+    __syncthreads();  // (the last piece's readers)
     for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
+    if (wave == 0) line_s[lane] = node_line(a.parents + first, n);
     __syncthreads();
-    dma(0, kl0, vl0);
-  }
 
-  if (__any(odd)) {
-    // such values make the sums of the rows that see them infinite or NaN,
-    // whatever their weights
-    for (int pos = max(base, pages0 * 16); pos < min(len, pages1 * 16); ++pos) {
-      const uint16_t *v = vbase + ((size_t)ptab[pos >> 4] * n_kv + g) * PB + (pos & 15);
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const uint16_t x = v[(16 * c + 4 * gq + d) * 16];
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-            if ((x & 0x7f80) == 0x7f80 && ((line[rt] >> (pos - base)) & 1)) acc[rt][c][d] += bf2f(x);
+    // K row j of a page holds its 16-byte chunk c at c ^ kswz(j): the score operand
+    // reads rows {0..3, 8..11} (or {4..7, 12..15}) of both pages at one chunk
+    // without bank conflicts.  V rows (one dimension, 32 bytes) need no swizzle.
+    auto kswz = [](int row) { return ((row & 3) | ((row >> 3) << 2)) << 1; };
+    const uint16_t *kbase = (const uint16_t *)a.kv.k, *vbase = (const uint16_t *)a.kv.v;
+    // A stage is 64 loads of 1 KB, four of K and four of V a page: each wave takes
+    // 64 / NW.  Pages past the split's last re-read it (never used unmasked).
+    auto dma = [&](int st, uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
+  #pragma unroll
+      for (int p = 0; p < SP / NW; ++p) {
+        const int page = wave * (SP / NW) + p;
+        const int phys = __builtin_amdgcn_readfirstlane(pid_s[min(st * SP + page, npg - 1)]);
+        const size_t at = ((size_t)phys * n_kv + g) * PB;
+  #pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int row = 4 * j + (lane >> 4);
+          __builtin_amdgcn_global_load_lds((const void *)(kbase + at + row * DH + ((lane & 15) ^ kswz(row)) * 8),
+                                           (lds_void *)(kb + page * PB + 4 * j * DH), 16, 0, 0);
         }
-    }
-  }
-  // the KW shares of a row: sums scaled to the common maximum and added in order
-  if constexpr (KW > 1) {
-    __syncthreads();
-    constexpr int PER = 4 / RT;  // waves' accumulators (8 KB a tile) per 32 KB array
-    float4 *const area[4] = {(float4 *)kl0, (float4 *)vl0, (float4 *)kl1, (float4 *)vl1};
-    static_assert((KW - 1) * RW <= 4 * PER, "the stage buffers hold the shares");
-    if (kw > 0) {
-      const int k = (kw - 1) * RW + rw;
-      float4 *to = (k / PER == 0 ? area[0] : k / PER == 1 ? area[1] : k / PER == 2 ? area[2] : area[3]) + (k % PER) * (RT * 512);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-          to[(rt * 8 + c) * 64 + lane] = make_float4(acc[rt][c][0], acc[rt][c][1], acc[rt][c][2], acc[rt][c][3]);
-    }
-    if (gq == 0)
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        ms[kw][rw * RT + rt][r] = m_run[rt];
-        ls[kw][rw * RT + rt][r] = acc_l[rt][0];
+  #pragma unroll
+        for (int j = 0; j < 4; ++j)
+          __builtin_amdgcn_global_load_lds((const void *)(vbase + at + 32 * j * 16 + lane * 8),
+                                           (lds_void *)(vb + page * PB + 32 * j * 16), 16, 0, 0);
       }
-    __syncthreads();
-    if (kw > 0) continue;
-#pragma unroll
+    };
+
+    dma(0, kl0, vl0);  // (the queries' loads run beside it)
+
+    const int wrow = row0 + rw * RT * 16;  // the wave's first row
+    u32x4 qf[RT][4];
+    uint64_t line[RT];
+  #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      float mx = kNoScore;
-#pragma unroll
-      for (int k = 0; k < KW; ++k) mx = fmaxf(mx, ms[k][rw * RT + rt][r]);
-      const float f0 = __builtin_amdgcn_exp2f(m_run[rt] - mx);
-      m_run[rt] = mx;
-      acc_l[rt] = acc_l[rt] * f0;
-#pragma unroll
-      for (int c = 0; c < 8; ++c) acc[rt][c] = acc[rt][c] * f0;
-#pragma unroll
-      for (int k = 1; k < KW; ++k) {
-        const int q = (k - 1) * RW + rw;
-        const float4 *from = (q / PER == 0 ? area[0] : q / PER == 1 ? area[1] : q / PER == 2 ? area[2] : area[3]) + (q % PER) * (RT * 512);
-        const float f = __builtin_amdgcn_exp2f(ms[k][rw * RT + rt][r] - mx);
-        acc_l[rt][0] += ls[k][rw * RT + rt][r] * f;
-#pragma unroll
+      const int rho = wrow + rt * 16 + r;
+      const bool live = rho < rows;
+      line[rt] = live ? line_s[rho / (G * a.np)] : 0;
+      const QT *qp = (const QT *)a.Q + place(live ? rho : 0) * DH + gq * 8;
+  #pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        if constexpr (sizeof(QT) == 2) {
+          qf[rt][s] = *(const u32x4 *)(qp + s * 32);
+        } else {  // the projections' queries, rounded once to the cache's type as in a step
+          const float4 x = *(const float4 *)(qp + s * 32), y = *(const float4 *)(qp + s * 32 + 4);
+          qf[rt][s] = u32x4{pack2(x.x, x.y), pack2(x.z, x.w), pack2(y.x, y.y), pack2(y.z, y.w)};
+        }
+        if (!live) qf[rt][s] = u32x4{0, 0, 0, 0};
+      }
+    }
+
+    float m_run[RT];
+    floatx4 acc[RT][8], acc_l[RT];  // acc_l: the sums of the rounded probabilities, by one more value multiply with V = 1
+    const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+  #pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      m_run[rt] = kNoScore;
+      acc_l[rt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  #pragma unroll
+      for (int c = 0; c < 8; ++c) acc[rt][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int kpage = r >> 3, kpos = 8 * ((r >> 2) & 1) + (r & 3);
+    const int vpage = gq >> 1, vpos = 8 * (gq & 1);
+    const bool active = wrow < rows;
+    bool odd = false;  // some node's value is not finite
+
+    auto pair = [&](int pg0, const uint16_t *kb, const uint16_t *vb, auto masked) __attribute__((always_inline)) {
+      constexpr bool MASKED = decltype(masked)::value;
+      u32x4 ka[4], kc[4], vf[8];
+  #pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        ka[s] = *(const u32x4 *)&kb[(kpage * 16 + kpos) * DH + ((s * 4 + gq) ^ kswz(kpos)) * 8];
+        kc[s] = *(const u32x4 *)&kb[(kpage * 16 + kpos + 4) * DH + ((s * 4 + gq) ^ kswz(kpos + 4)) * 8];
+      }
+      floatx4 sc[RT][2];
+  #pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        sc[rt][0] = sc[rt][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+  #pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          sc[rt][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka[s]),
+                                                              __builtin_bit_cast(bf16x8, qf[rt][s]), sc[rt][0], 0, 0, 0);
+          sc[rt][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kc[s]),
+                                                              __builtin_bit_cast(bf16x8, qf[rt][s]), sc[rt][1], 0, 0, 0);
+        }
+      }
+  #pragma unroll
+      for (int c = 0; c < 8; ++c) vf[c] = *(const u32x4 *)&vb[(vpage * DH + c * 16 + r) * 16 + vpos];
+      const int kp0 = (pb + pg0 + vpage) * 16 + vpos;  // position of this lane's first score
+      const bool page_ok = pg0 + vpage < npg;
+      if (MASKED) {
+        // slots past the sequence may hold anything; a node's values that are not
+        // finite would reach the rows that do not see it as 0 * infinity, so
+        // they are taken out here and added at the end
+  #pragma unroll
         for (int c = 0; c < 8; ++c) {
-          const float4 o = from[(rt * 8 + c) * 64 + lane];
-          acc[rt][c][0] += o.x * f;
-          acc[rt][c][1] += o.y * f;
-          acc[rt][c][2] += o.z * f;
-          acc[rt][c][3] += o.w * f;
+          vf[c] = mask8(vf[c], kp0, page_ok ? len : kp0);
+  #pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t x = vf[c][w];
+            const bool lo = (x & 0x7f80u) == 0x7f80u && kp0 + 2 * w >= base;
+            const bool hi = (x & 0x7f800000u) == 0x7f800000u && kp0 + 2 * w + 1 >= base;
+            odd |= lo | hi;
+            vf[c][w] = x & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
+          }
+        }
+      }
+      // (the row tiles' steps side by side: one tile alone leaves the units waiting
+      // for its chain of maximum, exponentials and conversion)
+      float s[RT][8], m_new[RT];
+      bool grow = false;
+  #pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+  #pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[rt][e] = sc[rt][0][e];
+          s[rt][4 + e] = sc[rt][1][e];
+        }
+        if (MASKED) {  // the row's eight positions: before `base`, or on its line
+          const int rel = kp0 - base;
+          const uint32_t seen = !page_ok || rel >= 64 ? 0u
+                                : rel >= 0            ? (uint32_t)(line[rt] >> rel) & 0xff
+                                : rel > -8            ? (uint32_t)((line[rt] << -rel) | ((1u << -rel) - 1)) & 0xff
+                                                      : 0xffu;
+  #pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (!((seen >> e) & 1)) s[rt][e] = -INFINITY;
+        }
+        float mt = s[rt][0];
+  #pragma unroll
+        for (int e = 1; e < 8; ++e) mt = fmaxf(mt, s[rt][e]);
+        // lazy rescaling: a row's base moves only when the pair's maximum exceeds it
+        // by more than kLazyMargin, so exponentials stay <= 2^kLazyMargin
+        const float mt_s = rows4_max(mt) * scale;
+        const bool up = mt_s > m_run[rt] + kLazyMargin;
+        m_new[rt] = up ? mt_s : m_run[rt];
+        grow |= up;
+      }
+      if (__any(grow)) {  // (a factor of exactly 1 where the base stays)
+  #pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const float corr = __builtin_amdgcn_exp2f(m_run[rt] - m_new[rt]);
+          acc_l[rt] = acc_l[rt] * corr;
+  #pragma unroll
+          for (int c = 0; c < 8; ++c) acc[rt][c] = acc[rt][c] * corr;
+          m_run[rt] = m_new[rt];
+        }
+      }
+      u32x4 pf[RT];
+  #pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float p[8];
+  #pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][e], scale, -m_new[rt]));
+        // (probabilities are rounded to bf16 for the matrix unit; their sum is of the rounded ones)
+        pf[rt] = u32x4{pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7])};
+      }
+  #pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        acc_l[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones),
+                                                            __builtin_bit_cast(bf16x8, pf[rt]), acc_l[rt], 0, 0, 0);
+  #pragma unroll
+        for (int c = 0; c < 8; ++c)
+          acc[rt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[c]),
+                                                               __builtin_bit_cast(bf16x8, pf[rt]), acc[rt][c], 0, 0, 0);
+      }
+    };
+    auto stage = [&](int st, const uint16_t *kb, const uint16_t *vb, auto masked) __attribute__((always_inline)) {
+      if (!active) return;
+  #pragma unroll 1
+      for (int j = 0; j < PP; ++j) {
+        const int pi = kw * PP + j, pg0 = st * SP + 2 * pi;
+        if (decltype(masked)::value && pg0 >= npg) break;
+        pair(pg0, kb + 2 * pi * PB, vb + 2 * pi * PB, masked);
+      }
+    };
+    // The barrier in front of a stage waits for its loads and for the readers of
+    // the other set, which the next stage's loads then fill.  Stages of which
+    // every row sees every key first, in pairs so that each set is known; then
+    // the last ones, those from the page of position `base` on.
+    for (;;) {
+      const int nst = (npg + SP - 1) / SP, nfull = max(0, min(npg, (base >> 4) - pb)) / SP;
+      for (int st = 0; st < nfull; st += 2) {
+        __syncthreads();
+        if (st + 1 < nst) dma(st + 1, kl1, vl1);
+        __builtin_amdgcn_sched_barrier(0);
+        stage(st, kl0, vl0, std::false_type{});
+        if (st + 1 < nfull) {
+          __syncthreads();
+          if (st + 2 < nst) dma(st + 2, kl0, vl0);
+          __builtin_amdgcn_sched_barrier(0);
+          stage(st + 1, kl1, vl1, std::false_type{});
+        }
+      }
+  #pragma unroll 1
+      for (int st = nfull; st < nst; ++st) {
+        __syncthreads();
+        const bool set1 = st & 1;
+        if (st + 1 < nst) dma(st + 1, set1 ? kl0 : kl1, set1 ? vl0 : vl1);
+        stage(st, set1 ? kl1 : kl0, set1 ? vl1 : vl0, std::true_type{});
+      }
+      pb += kWindow * 8;
+      if (pb >= pages1) break;
+      npg = min(pages1 - pb, kWindow * 8);
+      __syncthreads();
+      for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
+      __syncthreads();
+      dma(0, kl0, vl0);
+    }
+
+    if (__any(odd)) {
+      // such values make the sums of the rows that see them infinite or NaN,
+      // whatever their weights
+      for (int pos = max(base, pages0 * 16); pos < min(len, pages1 * 16); ++pos) {
+        const uint16_t *v = vbase + ((size_t)ptab[pos >> 4] * n_kv + g) * PB + (pos & 15);
+  #pragma unroll
+        for (int c = 0; c < 8; ++c)
+  #pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const uint16_t x = v[(16 * c + 4 * gq + d) * 16];
+  #pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+              if ((x & 0x7f80) == 0x7f80 && ((line[rt] >> (pos - base)) & 1)) acc[rt][c][d] += bf2f(x);
+          }
+      }
+    }
+    // the KW shares of a row: sums scaled to the common maximum and added in order
+    if constexpr (KW > 1) {
+      __syncthreads();
+      constexpr int PER = 4 / RT;  // waves' accumulators (8 KB a tile) per 32 KB array
+      float4 *const area[4] = {(float4 *)kl0, (float4 *)vl0, (float4 *)kl1, (float4 *)vl1};
+      static_assert((KW - 1) * RW <= 4 * PER, "the stage buffers hold the shares");
+      if (kw > 0) {
+        const int k = (kw - 1) * RW + rw;
+        float4 *to = (k / PER == 0 ? area[0] : k / PER == 1 ? area[1] : k / PER == 2 ? area[2] : area[3]) + (k % PER) * (RT * 512);
+  #pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+  #pragma unroll
+          for (int c = 0; c < 8; ++c)
+            to[(rt * 8 + c) * 64 + lane] = make_float4(acc[rt][c][0], acc[rt][c][1], acc[rt][c][2], acc[rt][c][3]);
+      }
+      if (gq == 0)
+  #pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          ms[kw][rw * RT + rt][r] = m_run[rt];
+          ls[kw][rw * RT + rt][r] = acc_l[rt][0];
+        }
+      __syncthreads();
+      if (kw > 0) continue;
+  #pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float mx = kNoScore;
+  #pragma unroll
+        for (int k = 0; k < KW; ++k) mx = fmaxf(mx, ms[k][rw * RT + rt][r]);
+        const float f0 = __builtin_amdgcn_exp2f(m_run[rt] - mx);
+        m_run[rt] = mx;
+        acc_l[rt] = acc_l[rt] * f0;
+  #pragma unroll
+        for (int c = 0; c < 8; ++c) acc[rt][c] = acc[rt][c] * f0;
+  #pragma unroll
+        for (int k = 1; k < KW; ++k) {
+          const int q = (k - 1) * RW + rw;
+          const float4 *from = (q / PER == 0 ? area[0] : q / PER == 1 ? area[1] : q / PER == 2 ? area[2] : area[3]) + (q % PER) * (RT * 512);
+          const float f = __builtin_amdgcn_exp2f(ms[k][rw * RT + rt][r] - mx);
+          acc_l[rt][0] += ls[k][rw * RT + rt][r] * f;
+  #pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            const float4 o = from[(rt * 8 + c) * 64 + lane];
+            acc[rt][c][0] += o.x * f;
+            acc[rt][c][1] += o.y * f;
+            acc[rt][c][2] += o.z * f;
+            acc[rt][c][3] += o.w * f;
+          }
         }
       }
     }
-  }
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int rho = wrow + rt * 16 + r;
-    if (rho >= rows) continue;
-    if (pc.is_whole()) {
-      const float inv = 1.f / acc_l[rt][0];
-      uint16_t *o = (uint16_t *)a.O + place(rho) * DH + 4 * gq;
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        *(u32x2 *)(o + 16 * c) = u32x2{pack2(acc[rt][c][0] * inv, acc[rt][c][1] * inv), pack2(acc[rt][c][2] * inv, acc[rt][c][3] * inv)};
-    } else {
-      const size_t to = ((size_t)pc.slot(w) * a.blocks + blk) * a.block + rho - row0;
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        *(float4 *)(a.opart + to * DH + 16 * c + 4 * gq) = make_float4(acc[rt][c][0], acc[rt][c][1], acc[rt][c][2], acc[rt][c][3]);
-      if (gq == 0) *(float2 *)(a.ostat + to * 2) = make_float2(m_run[rt], acc_l[rt][0]);
+  #pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int rho = wrow + rt * 16 + r;
+      if (rho >= rows) continue;
+      if (pc.is_whole()) {
+        const float inv = 1.f / acc_l[rt][0];
+        uint16_t *o = (uint16_t *)a.O + place(rho) * DH + 4 * gq;
+  #pragma unroll
+        for (int c = 0; c < 8; ++c)
+          *(u32x2 *)(o + 16 * c) = u32x2{pack2(acc[rt][c][0] * inv, acc[rt][c][1] * inv), pack2(acc[rt][c][2] * inv, acc[rt][c][3] * inv)};
+      } else {
+        const size_t to = ((size_t)pc.slot(w) * a.blocks + blk) * a.block + rho - row0;
+  #pragma unroll
+        for (int c = 0; c < 8; ++c)
+          *(float4 *)(a.opart + to * DH + 16 * c + 4 * gq) = make_float4(acc[rt][c][0], acc[rt][c][1], acc[rt][c][2], acc[rt][c][3]);
+        if (gq == 0) *(float2 *)(a.ostat + to * 2) = make_float2(m_run[rt], acc_l[rt][0]);
+      }
     }
-  }
   }
 }
 

@@ -131,6 +131,16 @@ def test_nearly_flat_rows(spread):
     check(z, None, None, rng.random(len(z)).astype(np.float32), kinds * 2)
 
 
+@pytest.mark.parametrize("nb", [0, 1])
+@pytest.mark.parametrize("min_p", [1e-6, 0.02, 0.3, 0.7, 1.0])
+def test_min_p_before_between_and_behind_the_other_cuts(min_p, nb):
+    rng = np.random.default_rng(12)
+    V, kinds = 20000, [(1.0, 700, 1.0, min_p), (1.0, 700, 0.5, min_p), (1.0, 0, 0.6, min_p), (1.5, 9000, 0.05, min_p),
+                       (1.0, 1, 1.0, min_p), (0.7, 12000, 0.99, min_p), (1.0, 0, 1.0, min_p)]
+    z1, zb, alpha = logits(rng, 2 * len(kinds), V, nb)
+    check(z1, zb, alpha, rng.random(len(z1)).astype(np.float32), kinds * 2)
+
+
 def test_masked_tokens_are_never_drawn():
     rng = np.random.default_rng(4)
     V, R = 5000, 3 * len(KINDS)

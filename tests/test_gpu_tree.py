@@ -160,6 +160,36 @@ def test_cache_beyond_one_splits_page_ids(dtype, nq, nkv, dh):
     c.sess.close()
 
 
+@pytest.mark.parametrize("paths,nodes", [(4, [64, 50]), (1, [4, 1])])
+def test_more_than_1024_pages_in_one_workgroup(paths, nodes):
+    """A sequence so long that the sixteen workgroups it is cut for have more
+    pages than they keep the numbers of.  A few rows in float64; the sums of n
+    keys take up to n more roundings in fp32."""
+    lens = [270000, 100]
+    c = Cache("bf16", 4, 1, 128, [a + b for a, b in zip(lens, nodes)], branches=3)
+    c.fill()
+    rng = np.random.default_rng(3)
+    parents = [p for n in nodes for p in random_tree(rng, n)]
+    q = torch.randn((paths, sum(nodes), 4, 128), generator=torch.Generator().manual_seed(4)).to(c.tt)
+    got = c.attend(nodes, parents, q)
+    assert torch.equal(got, c.attend(nodes, parents, q))
+    first = 0
+    for b, n in enumerate(nodes):
+        for i, line in enumerate(lines(parents[first:first + n])):
+            if i not in (0, 17, n - 1):
+                continue
+            pos = list(range(lens[b])) + sorted(lens[b] + j for j in line)
+            k, v = c.K[0][b][pos, 0].double(), c.V[0][b][pos, 0].double()
+            rows = [(p, h) for p in range(paths) for h in range(4)]
+            w = torch.softmax(torch.stack([q[p, first + i, h] for p, h in rows]).double() @ k.T / 128 ** 0.5, -1)
+            o, a = w @ v, w @ v.abs()
+            tol = 2.0 ** -8 * o.abs() + (2.02 * 2.0 ** -8 + len(pos) * 2.0 ** -24) * a
+            off = (torch.stack([got[p, first + i, h] for p, h in rows]).double() - o).abs() / tol
+            assert bool((off <= 1).all()), (b, i, float(off.max()))
+        first += n
+    c.sess.close()
+
+
 @pytest.mark.parametrize("batch", [130, 300])
 def test_more_sequences_than_one_launch_takes(batch):
     rng = np.random.default_rng(batch)
