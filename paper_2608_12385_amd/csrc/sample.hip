@@ -188,20 +188,26 @@ __device__ __forceinline__ void class_range(int c, int s, u64 &lo, u64 &hi) {
   hi = (u64)(9 + f) << sh;
 }
 
-__device__ __forceinline__ u64 wave_sum64(u64 v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+// Inclusive running sum over the wave's lanes (all of them active) without
+// LDS: shifts within each row of 16, then the rows' sums handed on.
+__device__ __forceinline__ u64 wave_scan64(u64 v) {
+  auto add = [](u64 x, auto ctrl, auto rows) {
+    const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, true);
+    const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(x >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xf, true);
+    return x + ((u64)hi << 32 | lo);
+  };
+  const std::integral_constant<int, 0xf> all{};
+  v = add(v, std::integral_constant<int, 0x111>{}, all);  // row_shr:1, 2, 4, 8
+  v = add(v, std::integral_constant<int, 0x112>{}, all);
+  v = add(v, std::integral_constant<int, 0x114>{}, all);
+  v = add(v, std::integral_constant<int, 0x118>{}, all);
+  v = add(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});  // row_bcast:15 to rows 1 and 3
+  return add(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});  // row_bcast:31 to rows 2 and 3
 }
-__device__ __forceinline__ u64 wave_scan64(u64 v) {  // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const u64 x = __shfl_up(v, o, 64);
-    if (lane >= o) v += x;
-  }
-  return v;
+__device__ __forceinline__ u64 lane64(u64 v, int lane) {  // lane: the same in every lane
+  return (u64)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, lane);
 }
+__device__ __forceinline__ u64 wave_sum64(u64 v) { return lane64(wave_scan64(v), 63); }
 // Sum and maximum over the block (red: 16 doubles; every thread gets the
 // result; fixed order).
 __device__ __forceinline__ double block_sum_d(double v, double *red) {
@@ -599,7 +605,7 @@ __device__ __forceinline__ void pick_bin(FinalShared &sh, u64 need, bool by_mass
     msum += m[k];
   }
   u64 before = wave_scan64(vs), mb = wave_scan64(msum) - msum;
-  need = min(need, __shfl(before, 63, 64));
+  need = min(need, lane64(before, 63));
   before -= vs;
   if (before < need && before + vs >= need) {
 #pragma unroll
@@ -716,17 +722,27 @@ __device__ __forceinline__ void cut_range(FinalShared &sh, const Listed &list, i
     sh.sum = above;
   }
   __syncthreads();
-  const int k = min(sh.n, kRankCap);
-  if (t < k) {
-    const u64 w = sh.rw[t];
-    const int ix = sh.ri[t];
-    u64 mass = 0;
-    unsigned rank = 0;
-    for (int o = 0; o < k; ++o)
+  // eight threads a token, each comparing it with an eighth of the others
+  const int k = min(sh.n, kRankCap), e = t >> 3;
+  static_assert(kRankCap * 8 == kFinal, "every token's eight threads");
+  u64 mass = 0, w = 0;
+  unsigned rank = 0;
+  int ix = 0;
+  if (e < k) {
+    w = sh.rw[e];
+    ix = sh.ri[e];
+    for (int o = t & 7; o < k; o += 8)
       if (sh.rw[o] > w || (sh.rw[o] == w && sh.ri[o] < ix)) {
         mass += sh.rw[o];
         ++rank;
       }
+  }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) {
+    mass += __shfl_xor(mass, o, 64);
+    rank += __shfl_xor(rank, o, 64);
+  }
+  if (e < k && (t & 7) == 0) {
     // the token before which less than need has come, and with which it is reached
     const u64 before = by_mass ? mass : rank, with = by_mass ? mass + w : rank + 1;
     if (before < need && with >= need) {
@@ -845,20 +861,22 @@ __global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
   __syncthreads();
   // the token: sums of every 256 neighbours by the waves, then the wave that
   // holds the target weighs its 256 again and finds the token
-  constexpr int PER = kTile / kFinal, RUN = PER * 64;
+  constexpr int PER = 4, RUN = PER * 64;
+  static_assert(RUN * NW == kTile, "a run per wave");
   const int p0 = sh.bin * a.part, n = min(a.V, p0 + a.part) - p0;
   before = sh.sum;
-  auto run = [&](int s0, u64 (&w)[PER]) __attribute__((always_inline)) {  // weights s0 + 64 k + lane that stay
-    float z[PER][NP];
+  auto run = [&](int s0, u64 (&w)[PER]) __attribute__((always_inline)) {  // this lane's four of the run's weights that stay
+    const int i = p0 + s0 + lane * PER;
+    float4u z[NP];
 #pragma unroll
-    for (int k = 0; k < PER; ++k)
-#pragma unroll
-      for (int j = 0; j < NP; ++j) z[k][j] = path_row(a, j, row)[p0 + min(s0 + k * 64 + lane, n - 1)];
+    for (int j = 0; j < NP; ++j) z[j] = load4(path_row(a, j, row), i, p0 + n);
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-      const int i = s0 + k * 64 + lane;
-      const u64 x = weight<NP>(r, z[k], a.s).w;
-      w[k] = i < n && (x > cut_w || (x == cut_w && p0 + i <= cut_i)) ? x : 0;
+      float zk[NP];
+#pragma unroll
+      for (int j = 0; j < NP; ++j) zk[j] = z[j][k];
+      const u64 x = weight<NP>(r, zk, a.s).w;
+      w[k] = x > cut_w || (x == cut_w && i + k <= cut_i) ? x : 0;
     }
   };
 #pragma unroll 2
@@ -878,21 +896,22 @@ __global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
   const u64 at = __ballot(target < runs);
   const int pick = __ffsll(at) - 1;  // (every wave agrees)
   if (pick >= 0 && pick % NW == wave) {
-    before = __shfl(runs - mine, pick, 64);
+    before = lane64(runs - mine, pick);
     const int s0 = pick / NW * kTile + wave * RUN;
-    u64 w[PER];
+    u64 w[PER], own = 0;
     run(s0, w);
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const u64 upto_i = before + wave_scan64(w[k]), end = __shfl(upto_i, 63, 64);
-      if (before <= target && target < end) {
-        const u64 hit = __ballot(upto_i > target);
-        if (lane == __ffsll(hit) - 1) {
-          a.token[row] = p0 + s0 + k * 64 + lane;
+    for (int k = 0; k < PER; ++k) own += w[k];
+    before += wave_scan64(own) - own;
+    if (before <= target && target < before + own) {
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        if (before <= target && target < before + w[k]) {
+          a.token[row] = p0 + s0 + lane * PER + k;
           if (a.prob) a.prob[row] = r.greedy ? 1.f : (float)((double)w[k] / (double)total);
         }
+        before += w[k];
       }
-      before = end;
     }
   }
 }
