@@ -208,27 +208,42 @@ __device__ __forceinline__ u64 lane64(u64 v, int lane) {  // lane: the same in e
   return (u64)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, lane);
 }
 __device__ __forceinline__ u64 wave_sum64(u64 v) { return lane64(wave_scan64(v), 63); }
-// Sum and maximum over the block (red: 16 doubles; every thread gets the
-// result; fixed order).
-__device__ __forceinline__ double block_sum_d(double v, double *red) {
+// Sums (MAX: maxima) of the wave's N values, in lane 63, by the same steps in
+// their fixed order.
+template <bool MAX, int N> __device__ __forceinline__ void wave_reduce_d(double (&v)[N]) {
+  auto step = [&](auto ctrl, auto rows) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  double t = 0;
-  for (int i = 0; i < (int)blockDim.x >> 6; ++i) t += red[i];
-  return t;
+    for (int k = 0; k < N; ++k) {
+      // (a lane without a partner: 0, or its own value)
+      const int lo = __double2loint(v[k]), hi = __double2hiint(v[k]);
+      const double o = __hiloint2double(
+          __builtin_amdgcn_update_dpp(MAX ? hi : 0, hi, decltype(ctrl)::value, decltype(rows)::value, 0xf, false),
+          __builtin_amdgcn_update_dpp(MAX ? lo : 0, lo, decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+      v[k] = MAX ? fmax(v[k], o) : v[k] + o;
+    }
+  };
+  const std::integral_constant<int, 0xf> all{};
+  step(std::integral_constant<int, 0x111>{}, all);
+  step(std::integral_constant<int, 0x112>{}, all);
+  step(std::integral_constant<int, 0x114>{}, all);
+  step(std::integral_constant<int, 0x118>{}, all);
+  step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+  step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
 }
-__device__ __forceinline__ double block_max_d(double v, double *red) {
+// The same over a row kernel's block, for every thread.
+template <bool MAX, int N> __device__ __forceinline__ void block_reduce_d(double (&v)[N], double (*red)[4]) {
+  wave_reduce_d<MAX>(v);
+  __syncthreads();  // (the last call's readers)
+  if ((threadIdx.x & 63) == 63)
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmax(v, __shfl_xor(v, o, 64));
+    for (int k = 0; k < N; ++k) red[threadIdx.x >> 6][k] = v[k];
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  double t = red[0];
-  for (int i = 1; i < (int)blockDim.x >> 6; ++i) t = fmax(t, red[i]);
-  return t;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    v[k] = red[0][k];
+#pragma unroll
+    for (int w = 1; w < kFinal / 64; ++w) v[k] = MAX ? fmax(v[k], red[w][k]) : v[k] + red[w][k];
+  }
 }
 
 // A row's parameters.  The greedy token is the first of the largest weight:
@@ -281,10 +296,13 @@ __global__ __launch_bounds__(256) void k_sample_stats(Args a, ParamBlock pb, int
         sum += k * 64 + lane < n ? e : 0.0;  // (values past the row repeat its last)
       }
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (NP > 1) {
+      double one[1] = {sum};
+      wave_reduce_d<false>(one);
+      sum = one[0];
+    }
     if (__any(bad)) sum = __longlong_as_double(0x7ff8000000000000ll);
-    if (lane == 0) a.w.stats[((size_t)row * a.tiles + tile) * 4 + j] = make_double2(mx, sum);
+    if (lane == 63) a.w.stats[((size_t)row * a.tiles + tile) * 4 + j] = make_double2(mx, sum);
   }
 }
 
@@ -294,8 +312,7 @@ __global__ __launch_bounds__(256) void k_sample_stats(Args a, ParamBlock pb, int
 // ub >= lb (less a margin over both sides' rounding) are evaluated.
 template <int NP>
 __global__ __launch_bounds__(kFinal) void k_sample_rows(Args a) {
-  __shared__ float red[16];
-  __shared__ double redd[16];
+  __shared__ double red[kFinal / 64][4];
   __shared__ int list[kMaxVocab / kTile];
   __shared__ int nlist;
   const int row = blockIdx.x, t = threadIdx.x;
@@ -305,17 +322,20 @@ __global__ __launch_bounds__(kFinal) void k_sample_rows(Args a) {
 #pragma unroll
   for (int j = 0; j < NP; ++j)
     st[j] = t < a.tiles ? a.w.stats[((size_t)row * a.tiles + t) * 4 + j] : make_double2(-INFINITY, 0.0);
-  float M[NP];
-  double S[NP], term[NP];
+  double M[NP], S[NP], term[NP];
   bool ok = true;
 #pragma unroll
+  for (int j = 0; j < NP; ++j) M[j] = st[j].x;
+  block_reduce_d<true>(M, red);
+#pragma unroll
   for (int j = 0; j < NP; ++j) {
-    M[j] = block_max((float)st[j].x, red);
     // (one path: the sums only say whether the row is sound)
-    term[j] = NP > 1 && t < a.tiles ? pow2((st[j].x - (double)M[j]) * kLog2eD) : 0.0;
-    S[j] = block_sum_d(NP > 1 && st[j].y > 0.0 ? st[j].y * term[j] : st[j].y, redd);
-    ok = ok && M[j] > -INFINITY && S[j] == S[j];
+    term[j] = NP > 1 && t < a.tiles ? pow2((st[j].x - M[j]) * kLog2eD) : 0.0;
+    S[j] = NP > 1 && st[j].y > 0.0 ? st[j].y * term[j] : st[j].y;
   }
+  block_reduce_d<false>(S, red);
+#pragma unroll
+  for (int j = 0; j < NP; ++j) ok = ok && M[j] > -INFINITY && S[j] == S[j];
   RowState rs;
   rs.scale[0] = 1.0;
   if (NP > 1) {
@@ -326,21 +346,21 @@ __global__ __launch_bounds__(kFinal) void k_sample_rows(Args a) {
     for (int j = 1; j < NP; ++j) rs.scale[j] = (1.0 - al) / (NP - 1) / S[j];
   }
 #pragma unroll
-  for (int j = 0; j < NP; ++j) rs.zmax[j] = M[j];
+  for (int j = 0; j < NP; ++j) rs.zmax[j] = (float)M[j];
   double mmax = 1.0;
   if (NP > 1 && ok) {
-    double lb = 0.0, ub = 0.0;
+    double lb[1] = {0.0}, ub = 0.0;
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       term[j] *= rs.scale[j];
-      lb = fmax(lb, term[j]);
+      lb[0] = fmax(lb[0], term[j]);
       ub += term[j];
     }
     if (t == 0) nlist = 0;
-    lb = block_max_d(lb, redd) * (1.0 - 1e-9);  // (its barriers come after the clearing)
-    if (t < a.tiles && ub >= lb) list[atomicAdd(&nlist, 1)] = t;  // (a maximum has no order)
+    block_reduce_d<true>(lb, red);  // (its barriers come after the clearing)
+    if (t < a.tiles && ub >= lb[0] * (1.0 - 1e-9)) list[atomicAdd(&nlist, 1)] = t;  // (a maximum has no order)
     __syncthreads();
-    double mx = 0.0;
+    double mx[1] = {0.0};
     // two tiles at a time, their loads in flight together (a last one twice)
     constexpr int N = kTile / kFinal;
     for (int n = 0; n < nlist; n += 2) {
@@ -351,15 +371,16 @@ __global__ __launch_bounds__(kFinal) void k_sample_rows(Args a) {
         for (int j = 0; j < NP; ++j)
           z[k][j] = path_row(a, j, row)[min(a.V - 1, list[min(n + k / N, nlist - 1)] * kTile + k % N * kFinal + t)];
 #pragma unroll
-      for (int k = 0; k < 2 * N; ++k) mx = fmax(mx, mixture<NP>(rs, z[k]));
+      for (int k = 0; k < 2 * N; ++k) mx[0] = fmax(mx[0], mixture<NP>(rs, z[k]));
     }
-    mmax = block_max_d(mx, redd);
+    block_reduce_d<true>(mx, red);
+    mmax = mx[0];
   }
   if (t == 0) {
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       r.scale[j] = rs.scale[j] / mmax;
-      r.zmax[j] = M[j];
+      r.zmax[j] = rs.zmax[j];
     }
     r.valid = ok;
   }
