@@ -576,25 +576,39 @@ __global__ __launch_bounds__(256) void k_sample_list(Args a) {
   __syncthreads();
   for (int i = lo + t * 16; i < hi; i += 256 * 16) {
     const u32x4 v = *(const u32x4 *)(cls + i);
+    const u64 half[2] = {(u64)v[1] << 32 | v[0], (u64)v[3] << 32 | v[2]};
+    unsigned m = 0;
 #pragma unroll
     for (int b = 0; b < 16; ++b) {
       const int c = (v[b >> 2] >> (8 * (b & 3))) & 0xff;
-      if ((unsigned)(c - r.l0) <= (unsigned)(r.l1 - r.l0) && ((c >= r.pl && c <= r.ph) || c == kc || c == r.lc) && i + b < hi)
-        idx[atomicAdd(&n_s, 1u)] = (uint16_t)(i + b - lo);
+      m |= (unsigned)(c - r.l0) <= (unsigned)(r.l1 - r.l0) ? 1u << b : 0u;
+    }
+    if (hi - i < 16) m &= (1u << (hi - i)) - 1;
+    for (unsigned k = m; k; k &= k - 1) {
+      const int b = __ffs(k) - 1, c = (half[b >> 3] >> (8 * (b & 7))) & 0xff;
+      if (!((c >= r.pl && c <= r.ph) || c == kc || c == r.lc)) m &= ~(1u << b);
+    }
+    if (m) {
+      unsigned at = atomicAdd(&n_s, (unsigned)__popc(m));
+      for (; m; m &= m - 1) idx[at++] = (uint16_t)(i + __ffs(m) - 1 - lo);
     }
   }
   __syncthreads();
-  const unsigned n = n_s;
-  if (t == 0 && n) at_s = atomicAdd(&a.w.state[row].listed, n);
-  __syncthreads();
-  for (unsigned k = t; k < n; k += 256) {
-    const int i = lo + idx[k];
-    float z[NP];
+  // (the first token of every thread is on its way before the list's place is known)
+  const int n = (int)n_s;
+  float z[NP];
+  auto fetch = [&](int k) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < NP; ++j) z[j] = path_row(a, j, row)[i];
+    for (int j = 0; j < NP; ++j) z[j] = path_row(a, j, row)[lo + idx[k]];
+  };
+  if (t < n) fetch(t);
+  if (t == 0 && n) at_s = atomicAdd(&a.w.state[row].listed, (unsigned)n);
+  __syncthreads();
+  for (int k = t; k < n; k += 256) {
+    if (k != t) fetch(k);
     const size_t o = (size_t)row * a.V + at_s + k;
     a.w.lw[o] = weight<NP>(r, z, a.s).w;
-    a.w.li[o] = i;
+    a.w.li[o] = lo + idx[k];
   }
 }
 
