@@ -90,6 +90,7 @@ __device__ __forceinline__ int schedule_place(int b, int n) {
 }
 
 typedef __attribute__((address_space(3))) void lds_void;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 constexpr int kWindow = 128;  // stages whose page ids are in LDS together
 
 // Growth of a row's score maximum (base 2) that moves its softmax base.
@@ -233,20 +234,28 @@ k_tree_attn_bf16(TreeAttn a) {
       const int kp0 = (pb + pg0 + vpage) * 16 + vpos;  // position of this lane's first score
       const bool page_ok = pg0 + vpage < npg;
       if (MASKED) {
-        // slots past the sequence may hold anything; a node's values that are not
-        // finite would reach the rows that do not see it as 0 * infinity, so
-        // they are taken out here and added at the end
-  #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          vf[c] = mask8(vf[c], kp0, page_ok ? len : kp0);
-  #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t x = vf[c][w];
-            const bool lo = (x & 0x7f80u) == 0x7f80u && kp0 + 2 * w >= base;
-            const bool hi = (x & 0x7f800000u) == 0x7f800000u && kp0 + 2 * w + 1 >= base;
-            odd |= lo | hi;
-            vf[c][w] = x & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
-          }
+        if ((pb + pg0 + 2) * 16 > len) {  // slots past the sequence may hold anything
+#pragma unroll
+          for (int c = 0; c < 8; ++c) vf[c] = mask8(vf[c], kp0, page_ok ? len : kp0);
+        }
+        // a node's values that are not finite would reach the rows that do not
+        // see it as 0 * infinity, so they are taken out here and added at the end
+        u16x2 top = {0, 0};
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[c][w] & 0x7fff7fffu));
+        if (__any(top.x >= 0x7f80 || top.y >= 0x7f80)) {
+#pragma unroll
+          for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const uint32_t x = vf[c][w];
+              const bool lo = (x & 0x7f80u) == 0x7f80u && kp0 + 2 * w >= base;
+              const bool hi = (x & 0x7f800000u) == 0x7f800000u && kp0 + 2 * w + 1 >= base;
+              odd |= lo | hi;
+              vf[c][w] = x & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
+            }
         }
       }
       // (the row tiles' steps side by side: one tile alone leaves the units waiting
