@@ -1451,7 +1451,7 @@ void schedule_tree(const dbt_config &c, int block, int blocks, TreeSeqs *g) {
   long long total = 0;
   int longest = 0;
   auto stages = [&](int i) {
-    const int pages = (g->base[i] + g->off[i + 1] - g->off[i] + kPage - 1) / kPage;
+    const int pages = (g->base[i] + g->nodes[i] + kPage - 1) / kPage;
     return (pages + kTreeStagePages - 1) / kTreeStagePages;
   };
   for (int i = 0; i < g->n; ++i) {
@@ -1466,6 +1466,19 @@ void schedule_tree(const dbt_config &c, int block, int blocks, TreeSeqs *g) {
   const long long cut = run * P + 2 * kTreeStart + block / kTreeMergeRows + kTreeMerge;
   g->whole = whole <= cut;
   g->per = g->whole ? 1 : (int)run;
+  if (g->whole) {
+    const TreeSeqs in = *g;
+    std::vector<int> order(g->n);
+    std::iota(order.begin(), order.end(), 0);
+    std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return stages(a) > stages(b); });
+    for (int i = 0; i < g->n; ++i) {
+      const int from = order[units > W ? i : i % 2 ? g->n - 1 - i / 2 : i / 2];
+      g->seq[i] = in.seq[from];
+      g->base[i] = in.base[from];
+      g->row[i] = in.row[from];
+      g->nodes[i] = in.nodes[from];
+    }
+  }
   g->first[0] = 0;
   for (int i = 0; i < g->n; ++i) g->first[i + 1] = g->first[i] + c.n_kv_heads * (g->whole ? 1 : stages(i));
 }
@@ -1491,13 +1504,13 @@ TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths
     if (p.groups.empty() || p.groups.back().n == kTreeSeqs) {
       p.groups.emplace_back();
       p.groups.back().n = 0;
-      p.groups.back().off[0] = off;
     }
     TreeSeqs &g = p.groups.back();
     g.seq[g.n] = b;
     g.base[g.n] = base[b];
+    g.row[g.n] = off;
+    g.nodes[g.n++] = n;
     off += n;
-    g.off[++g.n] = off;
   }
   for (TreeSeqs &g : p.groups) schedule_tree(cf, p.block, p.blocks, &g);
   return p;

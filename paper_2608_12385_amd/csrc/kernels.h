@@ -354,7 +354,7 @@ hipError_t launch_attn_prefill(const PromptAttn &a, hipStream_t st);
 
 // ---- drafted tokens (tree_attention.hip) ----
 // Sequences of a tree call that have nodes: sequence seq[i] has base[i]
-// positions before its nodes, which are rows off[i] .. off[i + 1] - 1 of the call.
+// positions before its nodes[i] nodes, which are rows row[i] .. of the call.
 //
 // The attention's work is units of one (sequence, KV head), sequence by
 // sequence; a unit is its pages in stages of kTreeStagePages.  Either every
@@ -367,7 +367,7 @@ constexpr int kTreeNodes = 64;  // DBT_TREE_NODES: one lane, one bit of a line o
 constexpr int kTreeStagePages = 8;
 struct TreeSeqs {
   int n, whole, per;
-  int seq[kTreeSeqs], base[kTreeSeqs], off[kTreeSeqs + 1], first[kTreeSeqs + 1];
+  int seq[kTreeSeqs], base[kTreeSeqs], row[kTreeSeqs], nodes[kTreeSeqs], first[kTreeSeqs + 1];
 };
 // Row map of the nodes (position, sequence, slot; kept nowhere).
 hipError_t launch_tree_rows(const TreeSeqs &s, const int *parents, PromptRow *rows, hipStream_t st);

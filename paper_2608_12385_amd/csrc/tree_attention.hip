@@ -30,7 +30,7 @@ __device__ __forceinline__ uint64_t node_line(const int *parents, int n) {
 }
 
 __global__ __launch_bounds__(64) void k_tree_rows(TreeSeqs s, const int *parents, PromptRow *rows) {
-  const int i = blockIdx.x, lane = threadIdx.x, first = s.off[i], n = s.off[i + 1] - first;
+  const int i = blockIdx.x, lane = threadIdx.x, first = s.row[i], n = s.nodes[i];
   const uint64_t line = node_line(parents + first, n);
   if (lane < n)
     ((int4 *)rows)[first + lane] = make_int4(s.base[i] + __popcll(line) - 1, s.seq[i], -1, s.base[i] + lane);
@@ -57,10 +57,10 @@ struct Piece {
   __device__ __forceinline__ int slot(int w) const { return 2 * w + (st0 == 0); }
 };
 __device__ __forceinline__ int seq_rows(const TreeAttn &a, int i) {
-  return (a.s.off[i + 1] - a.s.off[i]) * a.np * (a.n_q / a.kv.n_kv);
+  return a.s.nodes[i] * a.np * (a.n_q / a.kv.n_kv);
 }
 __device__ __forceinline__ int seq_stages(const TreeAttn &a, int i) {
-  const int pages = (a.s.base[i] + a.s.off[i + 1] - a.s.off[i] + 15) >> 4;
+  const int pages = (a.s.base[i] + a.s.nodes[i] + 15) >> 4;
   return (pages + kTreeStagePages - 1) / kTreeStagePages;
 }
 __device__ __forceinline__ Piece piece_at(const TreeAttn &a, int s, int end) {
@@ -133,7 +133,7 @@ k_tree_attn_bf16(TreeAttn a) {
     const Piece pc = piece_at(a, at, end);
     at += a.s.whole ? 1 : pc.st1 - pc.st0;
     const int i = pc.i, g = pc.g;
-    const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
+    const int first = a.s.row[i], n = a.s.nodes[i], base = a.s.base[i], len = base + n;
     const int rows = n * a.np * G, row0 = blk * (RW * RT * 16);
     if (row0 >= rows) continue;
     const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(64 * kWavesF32Attn) void k_tree_attn_f32(TreeAttn a
     const Piece pc = piece_at(a, s, end);
     s += a.s.whole ? 1 : pc.st1 - pc.st0;
     const int i = pc.i, g = pc.g;
-    const int first = a.s.off[i], n = a.s.off[i + 1] - first, base = a.s.base[i], len = base + n;
+    const int first = a.s.row[i], n = a.s.nodes[i], base = a.s.base[i], len = base + n;
     const int rows = n * a.np * G, row0 = blk * 16;
     if (row0 >= rows) continue;
     const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
@@ -494,7 +494,7 @@ __global__ __launch_bounds__(64 * kWavesF32Attn) void k_tree_attn_f32(TreeAttn a
 template <typename T>
 __global__ __launch_bounds__(256) void k_tree_combine(TreeAttn a) {
   const int i = blockIdx.z, g = blockIdx.y, DH = a.kv.d_h, Q4 = DH / 4;
-  const int first = a.s.off[i], rows = seq_rows(a, i), stages = seq_stages(a, i);
+  const int first = a.s.row[i], rows = seq_rows(a, i), stages = seq_stages(a, i);
   const int e = blockIdx.x * 256 + threadIdx.x, rho = e / Q4, d4 = e % Q4;
   if (rho >= rows) return;
   const int s0 = a.s.first[i] + g * stages;
