@@ -93,6 +93,14 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 constexpr int kWindow = 128;  // stages whose page ids are in LDS together
 
+// The barrier in front of a stage: every wave's loads into LDS have arrived
+// before any wave reads them (the compiler waits for a wave's own loads only,
+// and only in front of its own reads).
+__device__ __forceinline__ void stage_barrier() {
+  __builtin_amdgcn_s_waitcnt(0x70);  // vmcnt(0), lgkmcnt(0); expcnt not waited for
+  __syncthreads();
+}
+
 // Growth of a row's score maximum (base 2) that moves its softmax base.
 constexpr float kLazyMargin = 8.f;
 
@@ -334,12 +342,12 @@ k_tree_attn_bf16(TreeAttn a) {
     for (;;) {
       const int nst = (npg + SP - 1) / SP, nfull = max(0, min(npg, (base >> 4) - pb)) / SP;
       for (int st = 0; st < nfull; st += 2) {
-        __syncthreads();
+        stage_barrier();
         if (st + 1 < nst) dma(st + 1, kl1, vl1);
         __builtin_amdgcn_sched_barrier(0);
         stage(st, kl0, vl0, std::false_type{});
         if (st + 1 < nfull) {
-          __syncthreads();
+          stage_barrier();
           if (st + 2 < nst) dma(st + 2, kl0, vl0);
           __builtin_amdgcn_sched_barrier(0);
           stage(st + 1, kl1, vl1, std::false_type{});
@@ -347,7 +355,7 @@ k_tree_attn_bf16(TreeAttn a) {
       }
   #pragma unroll 1
       for (int st = nfull; st < nst; ++st) {
-        __syncthreads();
+        stage_barrier();
         const bool set1 = st & 1;
         if (st + 1 < nst) dma(st + 1, set1 ? kl0 : kl1, set1 ? vl0 : vl1);
         stage(st, set1 ? kl1 : kl0, set1 ? vl1 : vl0, std::true_type{});
