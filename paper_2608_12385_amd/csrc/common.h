@@ -68,6 +68,15 @@ __device__ __forceinline__ float wave_max_dpp(float x) {
   return rows4_max(x);
 }
 
+// The barrier in front of a stage that waves have sent for with loads straight
+// into LDS: every wave's loads have arrived before any wave reads them.  (The
+// compiler waits for a wave's own loads, in front of its own reads of an array
+// it sees them fill; __syncthreads alone waits for none.)
+__device__ __forceinline__ void stage_barrier() {
+  __builtin_amdgcn_s_waitcnt(0x70);  // vmcnt(0), lgkmcnt(0); expcnt not waited for
+  __syncthreads();
+}
+
 // Buffer resource over `bytes` bytes at p (raw, unswizzled, 32-bit data
 // format): a raw buffer load at an offset >= bytes returns zeros and reads no
 // memory, so a resource of zero bytes turns a wave's loads into no-ops without

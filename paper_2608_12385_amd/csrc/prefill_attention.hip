@@ -374,20 +374,20 @@ __global__ __launch_bounds__(1024) void k_attn_prefill_wide(PromptAttn a) {
 #pragma unroll
   for (int j = 0; j < SP; ++j) dma(j, kl0 + j * PB, vl0 + j * PB);
   for (int st = 0; st < nstages; st += 2) {
-    __syncthreads();
+    stage_barrier();
 #pragma unroll
     for (int j = 0; j < SP; ++j) dma((st + 1) * SP + j, kl1 + j * PB, vl1 + j * PB);
     __builtin_amdgcn_sched_barrier(0);
     stage(st, kl0, vl0);
     if (st + 1 < nstages) {  // uniform
-      __syncthreads();
+      stage_barrier();
 #pragma unroll
       for (int j = 0; j < SP; ++j) dma((st + 2) * SP + j, kl0 + j * PB, vl0 + j * PB);
       __builtin_amdgcn_sched_barrier(0);
       stage(st + 1, kl1, vl1);
     }
   }
-  __syncthreads();  // no load into LDS outlives the workgroup
+  stage_barrier();  // no load into LDS outlives the workgroup
   const float l_run = acc_l[0];
   if (qpos < T) {
     const float inv = 1.f / l_run;

@@ -93,14 +93,6 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 constexpr int kWindow = 128;  // stages whose page ids are in LDS together
 
-// The barrier in front of a stage: every wave's loads into LDS have arrived
-// before any wave reads them (the compiler waits for a wave's own loads only,
-// and only in front of its own reads).
-__device__ __forceinline__ void stage_barrier() {
-  __builtin_amdgcn_s_waitcnt(0x70);  // vmcnt(0), lgkmcnt(0); expcnt not waited for
-  __syncthreads();
-}
-
 // Growth of a row's score maximum (base 2) that moves its softmax base.
 constexpr float kLazyMargin = 8.f;
 
