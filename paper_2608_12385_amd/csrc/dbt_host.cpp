@@ -1369,7 +1369,7 @@ dbt_status decode_step_impl(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, int
 // unit (its stages take most of the LDS).  In pages of reading time (8 KB of keys
 // and values each): a piece's start, the merge's launch, and kTreeMergeRows rows' partial
 // results written and read (512 bytes each way).
-constexpr int kTreeStart = 6, kTreeMerge = 14, kTreeMergeRows = 8, kTreePieces = 16;
+constexpr int kTreeStart = 14, kTreeMerge = 14, kTreeMergeRows = 8, kTreePieces = 16;
 
 // may_be_empty: calls without a launch over the nodes
 dbt_status check_tree(const dbt_kv *kv, const dbt_tree *t, int *nodes, bool may_be_empty = false) {
@@ -1462,10 +1462,20 @@ void schedule_tree(const dbt_config &c, int block, int blocks, TreeSeqs *g) {
   // (a unit in at most kTreePieces pieces: the merge reads eight at a time)
   const long long rounds = (units + W - 1) / W, P = kTreeStagePages,
                   run = std::max<long long>((total + W - 1) / W, (longest + kTreePieces - 1) / kTreePieces);
+  long long part = longest;  // least run for which the units, each cut by itself, fit
+  for (long long lo = run; units <= W && lo < part;) {
+    const long long mid = (lo + part) / 2;
+    long long n = 0;
+    for (int i = 0; i < g->n; ++i) n += c.n_kv_heads * ((stages(i) + mid - 1) / mid);
+    if (n <= W) part = mid;
+    else lo = mid + 1;
+  }
+  const long long merge = block / kTreeMergeRows + kTreeMerge;
   const long long whole = (units <= W ? longest * P : std::max(longest * P, run * P + longest * P / 2)) + rounds * kTreeStart;
-  const long long cut = run * P + 2 * kTreeStart + block / kTreeMergeRows + kTreeMerge;
-  g->whole = whole <= cut;
-  g->per = g->whole ? 1 : (int)run;
+  const long long runs = run * P + 2 * kTreeStart + merge, parts = units <= W ? part * P + kTreeStart + merge : runs + 1;
+  g->whole = whole <= std::min(runs, parts);
+  g->per = g->whole ? 1 : (int)(parts <= runs ? part : run);
+  g->pad = !g->whole && parts <= runs ? g->per : 1;
   if (g->whole) {
     const TreeSeqs in = *g;
     std::vector<int> order(g->n);
@@ -1480,7 +1490,7 @@ void schedule_tree(const dbt_config &c, int block, int blocks, TreeSeqs *g) {
     }
   }
   g->first[0] = 0;
-  for (int i = 0; i < g->n; ++i) g->first[i + 1] = g->first[i] + c.n_kv_heads * (g->whole ? 1 : stages(i));
+  for (int i = 0; i < g->n; ++i) g->first[i + 1] = g->first[i] + c.n_kv_heads * (g->whole ? 1 : (stages(i) + g->pad - 1) / g->pad * g->pad);
 }
 
 // base[b]: positions of sequence b before its nodes.

@@ -359,14 +359,16 @@ hipError_t launch_attn_prefill(const PromptAttn &a, hipStream_t st);
 // The attention's work is units of one (sequence, KV head), sequence by
 // sequence; a unit is its pages in stages of kTreeStagePages.  Either every
 // workgroup takes a whole unit (whole), or all of them equal runs of `per`
-// stages of the units in a row, so that units are cut where runs end; first[i]
-// counts the units (whole) or stages before those of sequence i.  Query rows
-// beyond one workgroup's go to further workgroups with the same run.
+// stages of the units in a row, so that units are cut where runs end; units
+// may be rounded up to a multiple of `pad` stages (1, or `per`: no run goes
+// over a unit's end).  first[i] counts the units (whole) or stages before those of
+// sequence i.  Query rows beyond one workgroup's go to further workgroups with
+// the same run.
 constexpr int kTreeSeqs = 128;
 constexpr int kTreeNodes = 64;  // DBT_TREE_NODES: one lane, one bit of a line of ancestors each
 constexpr int kTreeStagePages = 8;
 struct TreeSeqs {
-  int n, whole, per;
+  int n, whole, per, pad;
   int seq[kTreeSeqs], base[kTreeSeqs], row[kTreeSeqs], nodes[kTreeSeqs], first[kTreeSeqs + 1];
 };
 // Row map of the nodes (position, sequence, slot; kept nowhere).

@@ -48,35 +48,49 @@ struct RowPlace {
 };
 
 // The next piece of work of run w at position s of the schedule (TreeSeqs):
-// stages st0 .. st1 - 1 of unit (sequence i, KV head g), which has `stages`.
+// stages st0 .. st1 - 1 of the `stages` of KV head g of a sequence (seq, whose
+// n nodes, rows first .., come after `base` positions).
 struct Piece {
-  int i, g, st0, st1, stages;
+  int seq, base, first, n, g, st0, st1, stages, next;  // next: position of the next piece
   __device__ __forceinline__ bool is_whole() const { return st0 == 0 && st1 == stages; }
   // A run has at most one piece that begins inside a unit (its first) and one
   // that begins a unit without ending it (its last).
   __device__ __forceinline__ int slot(int w) const { return 2 * w + (st0 == 0); }
 };
-__device__ __forceinline__ int seq_rows(const TreeAttn &a, int i) {
-  return a.s.nodes[i] * a.np * (a.n_q / a.kv.n_kv);
-}
-__device__ __forceinline__ int seq_stages(const TreeAttn &a, int i) {
-  const int pages = (a.s.base[i] + a.s.nodes[i] + 15) >> 4;
-  return (pages + kTreeStagePages - 1) / kTreeStagePages;
-}
+__device__ __forceinline__ int seq_rows(const TreeAttn &a, int i) { return a.s.nodes[i] * a.np * (a.n_q / a.kv.n_kv); }
+__device__ __forceinline__ int stages_of(int len) { return (((len + 15) >> 4) + kTreeStagePages - 1) / kTreeStagePages; }
+__device__ __forceinline__ int padded(const TreeSeqs &s, int stages) { return (stages + s.pad - 1) / s.pad * s.pad; }
 __device__ __forceinline__ Piece piece_at(const TreeAttn &a, int s, int end) {
-  // the sequence: as many of first[0 .. n) are at most s, counted by the wave
-  // (a search would wait for one argument after the other)
+  // as many of first[0 .. n) as are at most s lie before the sequence's end,
+  // counted by the wave: every lane brings one sequence's arguments (a search
+  // would wait for one argument after the other)
   const int lane = threadIdx.x & 63;
-  int lo = -1;
+  int lo = -1, first[kTreeSeqs / 64], seq[kTreeSeqs / 64], base[kTreeSeqs / 64], row[kTreeSeqs / 64], nodes[kTreeSeqs / 64];
 #pragma unroll
-  for (int k = 0; k < kTreeSeqs; k += 64) lo += __popcll(__ballot(k + lane < a.s.n && a.s.first[k + lane] <= s));
+  for (int k = 0; k < kTreeSeqs / 64; ++k) {
+    first[k] = a.s.first[k * 64 + lane];
+    seq[k] = a.s.seq[k * 64 + lane];
+    base[k] = a.s.base[k * 64 + lane];
+    row[k] = a.s.row[k * 64 + lane];
+    nodes[k] = a.s.nodes[k * 64 + lane];
+  }
+#pragma unroll
+  for (int k = 0; k < kTreeSeqs / 64; ++k) lo += __popcll(__ballot(k * 64 + lane < a.s.n && first[k] <= s));
+  auto its = [&](const int (&v)[kTreeSeqs / 64]) {
+    static_assert(kTreeSeqs == 128, "two sequences a lane");
+    return __builtin_amdgcn_readlane(lo >= 64 ? v[1] : v[0], lo & 63);
+  };
   Piece p;
-  p.i = lo;
-  p.stages = seq_stages(a, lo);
-  const int len = a.s.whole ? 1 : p.stages, rem = s - a.s.first[lo], unit = rem / len;
+  p.seq = its(seq);
+  p.base = its(base);
+  p.first = its(row);
+  p.n = its(nodes);
+  p.stages = stages_of(p.base + p.n);
+  const int len = a.s.whole ? 1 : padded(a.s, p.stages), rem = s - its(first), unit = rem / len;
   p.g = unit;
   p.st0 = a.s.whole ? 0 : rem % len;
   p.st1 = a.s.whole ? p.stages : min(p.stages, p.st0 + end - s);
+  p.next = s + (a.s.whole ? 1 : padded(a.s, p.st1 - p.st0));
   return p;
 }
 // Workgroups are dealt to the eight XCDs in turn: workgroup b takes a place that
@@ -131,68 +145,85 @@ k_tree_attn_bf16(TreeAttn a) {
   const int end = min(a.s.first[a.s.n], (w + 1) * a.s.per);
   for (int at = w * a.s.per; at < end;) {
     const Piece pc = piece_at(a, at, end);
-    at += a.s.whole ? 1 : pc.st1 - pc.st0;
-    const int i = pc.i, g = pc.g;
-    const int first = a.s.row[i], n = a.s.nodes[i], base = a.s.base[i], len = base + n;
+    at = pc.next;
+    const int g = pc.g, first = pc.first, n = pc.n, base = pc.base, len = base + n;
     const int rows = n * a.np * G, row0 = blk * (RW * RT * 16);
     if (row0 >= rows) continue;
     const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
-    const int *ptab = a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps;
+    const int *ptab = a.kv.page_table + (size_t)pc.seq * a.kv.mpps;
     const int pages0 = pc.st0 * 8, pages1 = min((len + 15) >> 4, pc.st1 * 8);  // the piece's pages
     int pb = pages0, npg = min(pages1 - pb, kWindow * 8);  // the window's first page, its pages
     __syncthreads();  // (the last piece's readers)
-    for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
-    if (wave == 0) line_s[lane] = node_line(a.parents + first, n);
-    __syncthreads();
 
     // K row j of a page holds its 16-byte chunk c at c ^ kswz(j): the score operand
     // reads rows {0..3, 8..11} (or {4..7, 12..15}) of both pages at one chunk
     // without bank conflicts.  V rows (one dimension, 32 bytes) need no swizzle.
     auto kswz = [](int row) { return ((row & 3) | ((row >> 3) << 2)) << 1; };
     const uint16_t *kbase = (const uint16_t *)a.kv.k, *vbase = (const uint16_t *)a.kv.v;
-    // A stage is 64 loads of 1 KB, four of K and four of V a page: each wave takes
-    // 64 / NW.  Pages past the split's last re-read it (never used unmasked).
-    auto dma = [&](int st, uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
-  #pragma unroll
+    // A stage is SP * 8 loads of 1 KB, four of K and four of V a page: each wave
+    // takes SP / NW pages.  Pages past the piece's last re-read it (never used unmasked).
+    auto dma = [&](const int (&phys)[SP / NW], uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
+#pragma unroll
       for (int p = 0; p < SP / NW; ++p) {
         const int page = wave * (SP / NW) + p;
-        const int phys = __builtin_amdgcn_readfirstlane(pid_s[min(st * SP + page, npg - 1)]);
-        const size_t at = ((size_t)phys * n_kv + g) * PB;
-  #pragma unroll
+        const size_t at = ((size_t)__builtin_amdgcn_readfirstlane(phys[p]) * n_kv + g) * PB;
+#pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int row = 4 * j + (lane >> 4);
           __builtin_amdgcn_global_load_lds((const void *)(kbase + at + row * DH + ((lane & 15) ^ kswz(row)) * 8),
                                            (lds_void *)(kb + page * PB + 4 * j * DH), 16, 0, 0);
         }
-  #pragma unroll
+#pragma unroll
         for (int j = 0; j < 4; ++j)
           __builtin_amdgcn_global_load_lds((const void *)(vbase + at + 32 * j * 16 + lane * 8),
                                            (lds_void *)(vb + page * PB + 32 * j * 16), 16, 0, 0);
       }
     };
-
-    dma(0, kl0, vl0);  // (the queries' loads run beside it)
-
+    auto next = [&](int st, uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
+      int phys[SP / NW];
+#pragma unroll
+      for (int p = 0; p < SP / NW; ++p) phys[p] = pid_s[min(st * SP + wave * (SP / NW) + p, npg - 1)];
+      dma(phys, kb, vb);
+    };
+    // Start: each wave finds its first stages' pages by itself and sends for them
+    // (for two stages where the piece is so short that the wait for each is a large
+    // part of its time); the other page ids, the lines and the queries come in
+    // meanwhile.  The first stage's barrier shows all of them.
     const int wrow = row0 + rw * RT * 16;  // the wave's first row
-    u32x4 qf[RT][4];
-    uint64_t line[RT];
-  #pragma unroll
+    int id[2][SP / NW], node[RT];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int p = 0; p < SP / NW; ++p) id[q][p] = ptab[pb + min(q * SP + wave * (SP / NW) + p, npg - 1)];
+    dma(id[0], kl0, vl0);
+    const int sent = npg > SP && npg <= 4 * SP ? 2 : 1;  // stages sent for
+    if (sent == 2) dma(id[1], kl1, vl1);
+    for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
+    if (wave == 0) line_s[lane] = node_line(a.parents + first, n);
+    constexpr int QW = sizeof(QT) / 2;
+    u32x4 raw[RT][4][QW];
+#pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const int rho = wrow + rt * 16 + r;
-      const bool live = rho < rows;
-      line[rt] = live ? line_s[rho / (G * a.np)] : 0;
-      const QT *qp = (const QT *)a.Q + place(live ? rho : 0) * DH + gq * 8;
-  #pragma unroll
+      const int rho = wrow + rt * 16 + r, own = rho < rows ? rho : 0;
+      node[rt] = own / (G * a.np);
+      const u32x4 *qp = (const u32x4 *)((const QT *)a.Q + place(own) * DH + gq * 8);
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int h = 0; h < QW; ++h) raw[rt][s][h] = qp[s * 4 * QW + h];
+    }
+    u32x4 qf[RT][4];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
       for (int s = 0; s < 4; ++s) {
-        if constexpr (sizeof(QT) == 2) {
-          qf[rt][s] = *(const u32x4 *)(qp + s * 32);
+        if constexpr (QW == 1) {
+          qf[rt][s] = raw[rt][s][0];
         } else {  // the projections' queries, rounded once to the cache's type as in a step
-          const float4 x = *(const float4 *)(qp + s * 32), y = *(const float4 *)(qp + s * 32 + 4);
+          const float4 x = __builtin_bit_cast(float4, raw[rt][s][0]), y = __builtin_bit_cast(float4, raw[rt][s][1]);
           qf[rt][s] = u32x4{pack2(x.x, x.y), pack2(x.z, x.w), pack2(y.x, y.y), pack2(y.z, y.w)};
         }
-        if (!live) qf[rt][s] = u32x4{0, 0, 0, 0};
       }
-    }
 
     float m_run[RT];
     floatx4 acc[RT][8], acc_l[RT];  // acc_l: the sums of the rounded probabilities, by one more value multiply with V = 1
@@ -271,9 +302,10 @@ k_tree_attn_bf16(TreeAttn a) {
         }
         if (MASKED) {  // the row's eight positions: before `base`, or on its line
           const int rel = kp0 - base;
+          const uint64_t line = line_s[node[rt]];
           const uint32_t seen = !page_ok || rel >= 64 ? 0u
-                                : rel >= 0            ? (uint32_t)(line[rt] >> rel) & 0xff
-                                : rel > -8            ? (uint32_t)((line[rt] << -rel) | ((1u << -rel) - 1)) & 0xff
+                                : rel >= 0            ? (uint32_t)(line >> rel) & 0xff
+                                : rel > -8            ? (uint32_t)((line << -rel) | ((1u << -rel) - 1)) & 0xff
                                                       : 0xffu;
   #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -320,7 +352,7 @@ k_tree_attn_bf16(TreeAttn a) {
     };
     auto stage = [&](int st, const uint16_t *kb, const uint16_t *vb, auto masked) __attribute__((always_inline)) {
       if (!active) return;
-  #pragma unroll 1
+#pragma unroll 1
       for (int j = 0; j < PP; ++j) {
         const int pi = kw * PP + j, pg0 = st * SP + 2 * pi;
         if (decltype(masked)::value && pg0 >= npg) break;
@@ -335,21 +367,21 @@ k_tree_attn_bf16(TreeAttn a) {
       const int nst = (npg + SP - 1) / SP, nfull = max(0, min(npg, (base >> 4) - pb)) / SP;
       for (int st = 0; st < nfull; st += 2) {
         stage_barrier();
-        if (st + 1 < nst) dma(st + 1, kl1, vl1);
+        if (st + 1 >= sent && st + 1 < nst) next(st + 1, kl1, vl1);
         __builtin_amdgcn_sched_barrier(0);
         stage(st, kl0, vl0, std::false_type{});
         if (st + 1 < nfull) {
           stage_barrier();
-          if (st + 2 < nst) dma(st + 2, kl0, vl0);
+          if (st + 2 < nst) next(st + 2, kl0, vl0);
           __builtin_amdgcn_sched_barrier(0);
           stage(st + 1, kl1, vl1, std::false_type{});
         }
       }
-  #pragma unroll 1
+#pragma unroll 1
       for (int st = nfull; st < nst; ++st) {
         stage_barrier();
         const bool set1 = st & 1;
-        if (st + 1 < nst) dma(st + 1, set1 ? kl0 : kl1, set1 ? vl0 : vl1);
+        if (st + 1 >= sent && st + 1 < nst) next(st + 1, set1 ? kl0 : kl1, set1 ? vl0 : vl1);
         stage(st, set1 ? kl1 : kl0, set1 ? vl1 : vl0, std::true_type{});
       }
       pb += kWindow * 8;
@@ -358,7 +390,7 @@ k_tree_attn_bf16(TreeAttn a) {
       __syncthreads();
       for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
       __syncthreads();
-      dma(0, kl0, vl0);
+      next(0, kl0, vl0);
     }
 
     if (__any(odd)) {
@@ -373,7 +405,7 @@ k_tree_attn_bf16(TreeAttn a) {
             const uint16_t x = v[(16 * c + 4 * gq + d) * 16];
   #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
-              if ((x & 0x7f80) == 0x7f80 && ((line[rt] >> (pos - base)) & 1)) acc[rt][c][d] += bf2f(x);
+              if ((x & 0x7f80) == 0x7f80 && ((line_s[node[rt]] >> (pos - base)) & 1)) acc[rt][c][d] += bf2f(x);
           }
       }
     }
@@ -459,9 +491,8 @@ __global__ __launch_bounds__(64 * kWavesF32Attn) void k_tree_attn_f32(TreeAttn a
   const int end = min(a.s.first[a.s.n], (w + 1) * a.s.per);
   for (int s = w * a.s.per; s < end;) {
     const Piece pc = piece_at(a, s, end);
-    s += a.s.whole ? 1 : pc.st1 - pc.st0;
-    const int i = pc.i, g = pc.g;
-    const int first = a.s.row[i], n = a.s.nodes[i], base = a.s.base[i], len = base + n;
+    s = pc.next;
+    const int g = pc.g, first = pc.first, n = pc.n, base = pc.base, len = base + n;
     const int rows = n * a.np * G, row0 = blk * 16;
     if (row0 >= rows) continue;
     const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
@@ -472,7 +503,7 @@ __global__ __launch_bounds__(64 * kWavesF32Attn) void k_tree_attn_f32(TreeAttn a
     const bool live = rho < rows;
     const SeesLine sees{base, live ? line_s[rho / (G * a.np)] : 0};
     attn_f32<NC>(mg, (const float *)a.Q + place(live ? rho : 0) * DH, live, sees, base >> 4, len, (const float *)a.kv.k,
-                 (const float *)a.kv.v, a.kv.page_table + (size_t)a.s.seq[i] * a.kv.mpps, pc.st0 * kTreeStagePages,
+                 (const float *)a.kv.v, a.kv.page_table + (size_t)pc.seq * a.kv.mpps, pc.st0 * kTreeStagePages,
                  min((len + 15) >> 4, pc.st1 * kTreeStagePages), a.kv.n_kv, g, DH);
     for (int e = threadIdx.x; e < min(16, rows - row0) * DH; e += 64 * kWavesF32Attn) {
       const int qr = e / DH, dh = e % DH;
@@ -494,10 +525,10 @@ __global__ __launch_bounds__(64 * kWavesF32Attn) void k_tree_attn_f32(TreeAttn a
 template <typename T>
 __global__ __launch_bounds__(256) void k_tree_combine(TreeAttn a) {
   const int i = blockIdx.z, g = blockIdx.y, DH = a.kv.d_h, Q4 = DH / 4;
-  const int first = a.s.row[i], rows = seq_rows(a, i), stages = seq_stages(a, i);
+  const int first = a.s.row[i], rows = seq_rows(a, i), stages = stages_of(a.s.base[i] + a.s.nodes[i]);
   const int e = blockIdx.x * 256 + threadIdx.x, rho = e / Q4, d4 = e % Q4;
   if (rho >= rows) return;
-  const int s0 = a.s.first[i] + g * stages;
+  const int s0 = a.s.first[i] + g * padded(a.s, stages);
   const int w0 = s0 / a.s.per, w1 = (s0 + stages - 1) / a.s.per;
   if (w0 == w1) return;  // written whole
   const RowPlace place{a.n_q / a.kv.n_kv, a.np, first, g, a.n_q, a.path_rows};
@@ -580,7 +611,7 @@ int tree_block_rows(int rows, int dtype) {
 
 hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st) {
   const int rows = a.max_nodes * a.np * (a.n_q / a.kv.n_kv);
-  if (a.s.n < 1 || a.s.n > kTreeSeqs || a.max_nodes < 1 || a.max_nodes > kTreeNodes || a.s.per < 1 ||
+  if (a.s.n < 1 || a.s.n > kTreeSeqs || a.max_nodes < 1 || a.max_nodes > kTreeNodes || a.s.per < 1 || a.s.pad < 1 ||
       a.block != tree_block_rows(rows, a.dtype) || a.blocks != (rows + a.block - 1) / a.block || (!a.s.whole && (!a.opart || !a.ostat)))
     return hipErrorInvalidValue;
   const dim3 grid((a.s.first[a.s.n] + a.s.per - 1) / a.s.per * a.blocks);
