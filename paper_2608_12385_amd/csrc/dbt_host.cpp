@@ -1365,10 +1365,10 @@ dbt_status decode_step_impl(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, int
 
 // ---- drafted tokens ----
 
-// How a tree's attention cuts its work (plan_tree).  A workgroup fills a compute
-// unit (its stages take most of the LDS).  In pages of reading time (8 KB of keys
-// and values each): a piece's start, the merge's launch, and kTreeMergeRows rows' partial
-// results written and read (512 bytes each way).
+// What a tree's attention costs beside its pages (schedule_tree), in pages of
+// reading time (8 KB of keys and values; 0.4 us for a workgroup while all read):
+// a piece's start, the merge's launch, and kTreeMergeRows rows' partial results
+// written and read.
 constexpr int kTreeStart = 14, kTreeMerge = 14, kTreeMergeRows = 8, kTreePieces = 16;
 
 // may_be_empty: calls without a launch over the nodes
@@ -1436,7 +1436,7 @@ TreeLayout tree_layout(const dbt_config &c, int nodes) {
   size_t slots = 0;  // in rows
   for (int r = 1; r <= rows; ++r) {
     const int block = tree_block_rows(r, c.dtype), blocks = (r + block - 1) / block;
-    slots = std::max(slots, (size_t)2 * std::max(1, tree_workgroups(block, c.dtype) / blocks) * blocks * block);
+    slots = std::max(slots, (size_t)2 * std::max(1, kTreeWorkgroups / blocks) * blocks * block);
   }
   L.map = 0;
   L.opart = align256((size_t)nodes * sizeof(PromptRow));
@@ -1445,8 +1445,16 @@ TreeLayout tree_layout(const dbt_config &c, int nodes) {
   return L;
 }
 
-// The schedule of up to kTreeSeqs sequences (see TreeSeqs): whole units, or equal
-// runs for one round of workgroups, whichever the estimate above makes shorter.
+// The schedule of up to kTreeSeqs sequences (see TreeSeqs): whole units, equal
+// runs for one round of workgroups, or units cut each by itself, whichever the
+// estimate makes shortest.  Measured (us; whole, runs, each by itself):
+//   8 KV heads, one sequence of 777, 96 rows         24.7  17.0  17.0
+//   one KV head, 13 of 150-4096, 32 rows             45.3  25.0  20.8
+//   8 KV heads, 8 of 16k-32k, 256 rows              694.5 285.5 289.7
+//   4 KV heads, 16 of 300-1500, 1024 rows            55.1  85.0  68.4
+// Whole units go longest first; where one round takes them all, long and short in
+// turns, which fall to one XCD and one compute unit together (the last line; 60 in
+// the sequences' order).
 void schedule_tree(const dbt_config &c, int block, int blocks, TreeSeqs *g) {
   long long total = 0;
   int longest = 0;
@@ -1458,7 +1466,7 @@ void schedule_tree(const dbt_config &c, int block, int blocks, TreeSeqs *g) {
     total += (long long)c.n_kv_heads * stages(i);
     longest = std::max(longest, stages(i));
   }
-  const long long units = (long long)g->n * c.n_kv_heads, W = std::max(1, tree_workgroups(block, c.dtype) / blocks);
+  const long long units = (long long)g->n * c.n_kv_heads, W = std::max(1, kTreeWorkgroups / blocks);
   // (a unit in at most kTreePieces pieces: the merge reads eight at a time)
   const long long rounds = (units + W - 1) / W, P = kTreeStagePages,
                   run = std::max<long long>((total + W - 1) / W, (longest + kTreePieces - 1) / kTreePieces);

@@ -391,9 +391,9 @@ struct TreeAttn {
 hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st);
 // Query rows of one workgroup where a sequence has up to `rows` for a KV head
 // (nodes x paths x query heads of the KV head).
-int tree_block_rows(int rows, int dtype);
-// Workgroups of the kernel for such blocks that run at a time.
-int tree_workgroups(int block, int dtype);
+inline int tree_block_rows(int rows, int dtype) { return dtype != 1 ? 16 : rows <= 64 ? 64 : 128; }
+// Workgroups of the kernels that run at a time: two a compute unit.
+constexpr int kTreeWorkgroups = 2 * kComputeUnits;
 // Kept nodes of up to kKeepSeqs sequences: node path[i][j] of sequence seq[i]
 // moves to position base[i] + j, j = first[i] .. count[i] - 1 (those before
 // stay where they are).

@@ -105,39 +105,44 @@ __device__ __forceinline__ int schedule_place(int b, int n) {
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-constexpr int kWindow = 128;  // stages whose page ids are in LDS together
+constexpr int kWindow = 1024;  // pages whose ids are in LDS together
 
 // Growth of a row's score maximum (base 2) that moves its softmax base.
 constexpr float kLazyMargin = 8.f;
 
-// bf16 cache, d_h = 128.  A workgroup owns RW * RT * 16 query rows of one
-// (sequence, KV head) and a split of its pages.  Eight pages a stage go straight
-// into LDS (64 KB), one stage ahead of the multiplies, so every key and value
-// is fetched once for all rows of the workgroup; wave (rw, kw) multiplies row
-// tiles rw * RT .. + RT - 1 with its share kw of the stage's page pairs, and the KW
-// shares are merged at the end.  Few rows: four waves share the keys (KW = 4,
-// one row tile each holds them all); many: eight waves share the rows.  The
-// arithmetic of a pair is that of the decode kernel: scores S = K Q^T with
-// permuted rows, so that lane (row r, group gq) ends up with eight
-// consecutive positions of one page, which is the operand of O^T = V^T P^T.
-// Rows see different keys only in pages from position `base` on; those pairs
-// take a masked path.
+// bf16 cache, d_h = 128.  A workgroup of four waves, two of them a compute
+// unit, owns 64 RT query rows of one (sequence, KV head) and a piece of its pages.
+// Four pages a stage (32 KB) go straight into LDS, one stage ahead of the
+// multiplies, so every key and value is fetched once for all rows of the
+// workgroup; wave w multiplies its RT row tiles of 16 with all of them.  The
+// arithmetic of a pair of pages is that of the decode kernel: scores S = K Q^T
+// with permuted rows, so that lane (row r, group gq) ends up with eight
+// consecutive positions of one page, which is the operand of O^T = V^T P^T; one
+// running maximum and sum a row.  Rows see different keys only in pages from
+// position `base` on; those pairs take a masked path.
 //
-// Bound: 16 rows and up to 128 per key read at the memory's rate; 256 rows by
-// the vector unit's softmax beside the matrix unit.
-template <int RT, int RW, int KW, int SP, typename QT>
-__global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(RW *KW * (SP == 4 ? 2 : 1) / 4, RW *KW * (SP == 4 ? 2 : 1) / 4))) void
-k_tree_attn_bf16(TreeAttn a) {
-  constexpr int DH = 128, NW = RW * KW, PP = SP / 2 / KW, PB = 16 * DH;  // PP: pairs of a stage per wave; PB: elements of a page
-  static_assert(kTreeStagePages % SP == 0 && KW * PP * 2 == SP && SP % NW == 0, "whole pairs and pages for every wave");
+// Up to 64 rows RT is 1, so that all four SIMDs have a part of them (32 x 4096
+// positions, eight KV heads: 97 us with 8 rows and 111 with 64; with RT = 2 two
+// SIMDs stand idle, 100 and 115); more rows are faster with two tiles a wave, whose
+// softmax steps run side by side and which read LDS half as often.  Eight
+// waves that also share a stage's pairs (merged at the end) take 107 us for those 64
+// rows but 142 against 111 for 48 x 200-4000, since nothing runs while the
+// compute unit's one workgroup begins its next piece.
+//
+// Bound: up to 64 rows the memory (97 us: 5.6 TB/s).  From 128 rows the matrix
+// unit beside the softmax: 16 x 300-1500 with 1024 rows 54 us, 3.1e10 operations
+// (the longest sequence alone takes 45); 8 x 16k-32k with 256 rows 285 us, 2.1e11
+// operations, 215 without the loads and 171 without the multiplies.
+template <int RT, typename QT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_tree_attn_bf16(TreeAttn a) {
+  constexpr int DH = 128, NW = 4, SP = 4, PB = 16 * DH;  // waves; pages of a stage; elements of a page
+  static_assert(SP == NW && kTreeStagePages % SP == 0, "a page per wave, whole stages");
   // two sets of stage buffers, separate arrays so that the loads filling one
   // set are told apart from the reads of the other
   __shared__ __attribute__((aligned(16))) uint16_t kl0[SP * PB], vl0[SP * PB], kl1[SP * PB], vl1[SP * PB];
-  __shared__ int pid_s[kWindow * kTreeStagePages];
+  __shared__ int pid_s[kWindow];
   __shared__ uint64_t line_s[kTreeNodes];
-  __shared__ float ms[KW][RW * RT][16], ls[KW][RW * RT][16];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int rw = wave % RW, kw = wave / RW;
   const int r = lane & 15, gq = lane >> 4;
   const int n_kv = a.kv.n_kv, G = a.n_q / n_kv;
   const float scale = kLog2e / sqrtf((float)DH);
@@ -147,12 +152,12 @@ k_tree_attn_bf16(TreeAttn a) {
     const Piece pc = piece_at(a, at, end);
     at = pc.next;
     const int g = pc.g, first = pc.first, n = pc.n, base = pc.base, len = base + n;
-    const int rows = n * a.np * G, row0 = blk * (RW * RT * 16);
+    const int rows = n * a.np * G, row0 = blk * (16 * RT * NW);
     if (row0 >= rows) continue;
     const RowPlace place{G, a.np, first, g, a.n_q, a.path_rows};
     const int *ptab = a.kv.page_table + (size_t)pc.seq * a.kv.mpps;
-    const int pages0 = pc.st0 * 8, pages1 = min((len + 15) >> 4, pc.st1 * 8);  // the piece's pages
-    int pb = pages0, npg = min(pages1 - pb, kWindow * 8);  // the window's first page, its pages
+    const int pages0 = pc.st0 * kTreeStagePages, pages1 = min((len + 15) >> 4, pc.st1 * kTreeStagePages);  // the piece's pages
+    int pb = pages0, npg = min(pages1 - pb, kWindow);  // the window's first page, its pages
     __syncthreads();  // (the last piece's readers)
 
     // K row j of a page holds its 16-byte chunk c at c ^ kswz(j): the score operand
@@ -160,47 +165,37 @@ k_tree_attn_bf16(TreeAttn a) {
     // without bank conflicts.  V rows (one dimension, 32 bytes) need no swizzle.
     auto kswz = [](int row) { return ((row & 3) | ((row >> 3) << 2)) << 1; };
     const uint16_t *kbase = (const uint16_t *)a.kv.k, *vbase = (const uint16_t *)a.kv.v;
-    // A stage is SP * 8 loads of 1 KB, four of K and four of V a page: each wave
-    // takes SP / NW pages.  Pages past the piece's last re-read it (never used unmasked).
-    auto dma = [&](const int (&phys)[SP / NW], uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
+    // A stage is eight loads of 1 KB a page, four of K and four of V: each wave
+    // takes one page.  Pages past the piece's last re-read it (never used unmasked).
+    auto dma = [&](int id, uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
+      const size_t at = ((size_t)__builtin_amdgcn_readfirstlane(id) * n_kv + g) * PB;
 #pragma unroll
-      for (int p = 0; p < SP / NW; ++p) {
-        const int page = wave * (SP / NW) + p;
-        const size_t at = ((size_t)__builtin_amdgcn_readfirstlane(phys[p]) * n_kv + g) * PB;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int row = 4 * j + (lane >> 4);
-          __builtin_amdgcn_global_load_lds((const void *)(kbase + at + row * DH + ((lane & 15) ^ kswz(row)) * 8),
-                                           (lds_void *)(kb + page * PB + 4 * j * DH), 16, 0, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          __builtin_amdgcn_global_load_lds((const void *)(vbase + at + 32 * j * 16 + lane * 8),
-                                           (lds_void *)(vb + page * PB + 32 * j * 16), 16, 0, 0);
+      for (int j = 0; j < 4; ++j) {
+        const int row = 4 * j + (lane >> 4);
+        __builtin_amdgcn_global_load_lds((const void *)(kbase + at + row * DH + ((lane & 15) ^ kswz(row)) * 8),
+                                         (lds_void *)(kb + wave * PB + 4 * j * DH), 16, 0, 0);
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        __builtin_amdgcn_global_load_lds((const void *)(vbase + at + 32 * j * 16 + lane * 8),
+                                         (lds_void *)(vb + wave * PB + 32 * j * 16), 16, 0, 0);
     };
     auto next = [&](int st, uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
-      int phys[SP / NW];
-#pragma unroll
-      for (int p = 0; p < SP / NW; ++p) phys[p] = pid_s[min(st * SP + wave * (SP / NW) + p, npg - 1)];
-      dma(phys, kb, vb);
+      dma(pid_s[min(st * SP + wave, npg - 1)], kb, vb);
     };
     // Start: each wave finds its first stages' pages by itself and sends for them
     // (for two stages where the piece is so short that the wait for each is a large
     // part of its time); the other page ids, the lines and the queries come in
     // meanwhile.  The first stage's barrier shows all of them.
-    const int wrow = row0 + rw * RT * 16;  // the wave's first row
-    int id[2][SP / NW], node[RT];
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-      for (int p = 0; p < SP / NW; ++p) id[q][p] = ptab[pb + min(q * SP + wave * (SP / NW) + p, npg - 1)];
-    dma(id[0], kl0, vl0);
+    const int wrow = row0 + wave * RT * 16;  // the wave's first row
+    const int id0 = ptab[pb + min(wave, npg - 1)], id1 = ptab[pb + min(SP + wave, npg - 1)];
+    dma(id0, kl0, vl0);
     const int sent = npg > SP && npg <= 4 * SP ? 2 : 1;  // stages sent for
-    if (sent == 2) dma(id[1], kl1, vl1);
+    if (sent == 2) dma(id1, kl1, vl1);
     for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
     if (wave == 0) line_s[lane] = node_line(a.parents + first, n);
     constexpr int QW = sizeof(QT) / 2;
+    int node[RT];
     u32x4 raw[RT][4][QW];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -353,10 +348,10 @@ k_tree_attn_bf16(TreeAttn a) {
     auto stage = [&](int st, const uint16_t *kb, const uint16_t *vb, auto masked) __attribute__((always_inline)) {
       if (!active) return;
 #pragma unroll 1
-      for (int j = 0; j < PP; ++j) {
-        const int pi = kw * PP + j, pg0 = st * SP + 2 * pi;
+      for (int j = 0; j < SP / 2; ++j) {
+        const int pg0 = st * SP + 2 * j;
         if (decltype(masked)::value && pg0 >= npg) break;
-        pair(pg0, kb + 2 * pi * PB, vb + 2 * pi * PB, masked);
+        pair(pg0, kb + 2 * j * PB, vb + 2 * j * PB, masked);
       }
     };
     // The barrier in front of a stage waits for its loads and for the readers of
@@ -384,9 +379,9 @@ k_tree_attn_bf16(TreeAttn a) {
         if (st + 1 >= sent && st + 1 < nst) next(st + 1, set1 ? kl0 : kl1, set1 ? vl0 : vl1);
         stage(st, set1 ? kl1 : kl0, set1 ? vl1 : vl0, std::true_type{});
       }
-      pb += kWindow * 8;
+      pb += kWindow;
       if (pb >= pages1) break;
-      npg = min(pages1 - pb, kWindow * 8);
+      npg = min(pages1 - pb, kWindow);
       __syncthreads();
       for (int k = t; k < npg; k += 64 * NW) pid_s[k] = ptab[pb + k];
       __syncthreads();
@@ -409,57 +404,7 @@ k_tree_attn_bf16(TreeAttn a) {
           }
       }
     }
-    // the KW shares of a row: sums scaled to the common maximum and added in order
-    if constexpr (KW > 1) {
-      __syncthreads();
-      constexpr int PER = 4 / RT;  // waves' accumulators (8 KB a tile) per 32 KB array
-      float4 *const area[4] = {(float4 *)kl0, (float4 *)vl0, (float4 *)kl1, (float4 *)vl1};
-      static_assert((KW - 1) * RW <= 4 * PER, "the stage buffers hold the shares");
-      if (kw > 0) {
-        const int k = (kw - 1) * RW + rw;
-        float4 *to = (k / PER == 0 ? area[0] : k / PER == 1 ? area[1] : k / PER == 2 ? area[2] : area[3]) + (k % PER) * (RT * 512);
-  #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-  #pragma unroll
-          for (int c = 0; c < 8; ++c)
-            to[(rt * 8 + c) * 64 + lane] = make_float4(acc[rt][c][0], acc[rt][c][1], acc[rt][c][2], acc[rt][c][3]);
-      }
-      if (gq == 0)
-  #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          ms[kw][rw * RT + rt][r] = m_run[rt];
-          ls[kw][rw * RT + rt][r] = acc_l[rt][0];
-        }
-      __syncthreads();
-      if (kw > 0) continue;
-  #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float mx = kNoScore;
-  #pragma unroll
-        for (int k = 0; k < KW; ++k) mx = fmaxf(mx, ms[k][rw * RT + rt][r]);
-        const float f0 = __builtin_amdgcn_exp2f(m_run[rt] - mx);
-        m_run[rt] = mx;
-        acc_l[rt] = acc_l[rt] * f0;
-  #pragma unroll
-        for (int c = 0; c < 8; ++c) acc[rt][c] = acc[rt][c] * f0;
-  #pragma unroll
-        for (int k = 1; k < KW; ++k) {
-          const int q = (k - 1) * RW + rw;
-          const float4 *from = (q / PER == 0 ? area[0] : q / PER == 1 ? area[1] : q / PER == 2 ? area[2] : area[3]) + (q % PER) * (RT * 512);
-          const float f = __builtin_amdgcn_exp2f(ms[k][rw * RT + rt][r] - mx);
-          acc_l[rt][0] += ls[k][rw * RT + rt][r] * f;
-  #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            const float4 o = from[(rt * 8 + c) * 64 + lane];
-            acc[rt][c][0] += o.x * f;
-            acc[rt][c][1] += o.y * f;
-            acc[rt][c][2] += o.z * f;
-            acc[rt][c][3] += o.w * f;
-          }
-        }
-      }
-    }
-  #pragma unroll
+#pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const int rho = wrow + rt * 16 + r;
       if (rho >= rows) continue;
@@ -600,15 +545,6 @@ hipError_t launch_tree_rows(const TreeSeqs &s, const int *parents, PromptRow *ro
   return hipGetLastError();
 }
 
-int tree_workgroups(int block, int dtype) { return dtype == 1 && block < 128 ? kComputeUnits : 2 * kComputeUnits; }
-
-int tree_block_rows(int rows, int dtype) {
-  if (dtype != 1) return 16;
-  for (int r = 16; r < 128; r *= 2)
-    if (rows <= r) return r;
-  return 128;
-}
-
 hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st) {
   const int rows = a.max_nodes * a.np * (a.n_q / a.kv.n_kv);
   if (a.s.n < 1 || a.s.n > kTreeSeqs || a.max_nodes < 1 || a.max_nodes > kTreeNodes || a.s.per < 1 || a.s.pad < 1 ||
@@ -617,17 +553,11 @@ hipError_t launch_tree_attn(const TreeAttn &a, hipStream_t st) {
   const dim3 grid((a.s.first[a.s.n] + a.s.per - 1) / a.s.per * a.blocks);
   if (a.dtype == 1) {
     if (a.kv.d_h != 128) return hipErrorInvalidValue;
-    auto go = [&](auto q) {
-      typedef decltype(q) QT;
-      switch (a.block) {
-        case 16: hipLaunchKernelGGL((k_tree_attn_bf16<1, 1, 4, 8, QT>), grid, dim3(256), 0, st, a); break;
-        case 32: hipLaunchKernelGGL((k_tree_attn_bf16<2, 1, 4, 8, QT>), grid, dim3(256), 0, st, a); break;
-        case 64: hipLaunchKernelGGL((k_tree_attn_bf16<2, 2, 4, 8, QT>), grid, dim3(512), 0, st, a); break;
-        default: hipLaunchKernelGGL((k_tree_attn_bf16<2, 4, 1, 4, QT>), grid, dim3(256), 0, st, a); break;
-      }
-    };
-    if (a.q32) go(float{});
-    else go(uint16_t{});
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
+    if (a.q32)
+      a.block == 64 ? go(k_tree_attn_bf16<1, float>) : go(k_tree_attn_bf16<2, float>);
+    else
+      a.block == 64 ? go(k_tree_attn_bf16<1, uint16_t>) : go(k_tree_attn_bf16<2, uint16_t>);
   } else {
     if (a.kv.d_h > 128) return hipErrorInvalidValue;
     const dim3 block(64 * kWavesF32Attn);
