@@ -141,6 +141,21 @@ def test_min_p_before_between_and_behind_the_other_cuts(min_p, nb):
     check(z1, zb, alpha, rng.random(len(z1)).astype(np.float32), kinds * 2)
 
 
+@pytest.mark.parametrize("nb", [0, 1, 2, 3])
+@pytest.mark.parametrize("t", [1e-3, 1e-7, 1e-13, 1e-30, 1e-45])
+def test_the_smallest_temperatures(t, nb):
+    """The largest weight stays one, whatever its logarithm is multiplied with:
+    those of the rows' seconds are below 2^-46 from 1e-3 on."""
+    rng = np.random.default_rng(13)
+    z1, zb, alpha = logits(rng, 12, 3000, nb)
+    z1[:, 100] += 60
+    if nb:
+        zb[:, :, 100] += 60
+    u = rng.random(12).astype(np.float32)
+    token, prob = call(z1, zb, alpha, u, [(t, 0, 1.0, 0.0), (t, 5, 0.9, 0.1)] * 6)
+    assert (token == 100).all() and (prob == 1).all()
+
+
 def test_masked_tokens_are_never_drawn():
     rng = np.random.default_rng(4)
     V, R = 5000, 3 * len(KINDS)
