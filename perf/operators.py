@@ -210,23 +210,43 @@ class _Cache:
         self.page_table = torch.full((c["batch"], self.mpps), -1, dtype=torch.int32, device="cuda")
         self.kv = binding.dbt_kv_create(self.model, self.k.data_ptr(), self.v.data_ptr(), self.num_pages,
                                         self.page_table.data_ptr(), self.mpps)
-        for b in range(c["batch"]):
+        # The library hands out the lowest free page first.  Sequences whose
+        # nodes are dropped and grown again stand in reverse, so that growing
+        # them in a row takes the pages of the table again.
+        B, keep = c["batch"], c["op"] == "keep"
+        at = [B - 1 - b if keep else b for b in range(B)]
+        for b in range(B):
             if half[b]:
-                binding.dbt_kv_reserve(self.kv, b, half[b] * PAGE)
-        for b in reversed(range(c["batch"])):
-            binding.dbt_kv_reserve(self.kv, b, total[b])
-        self.tree = binding.make_tree(self.nodes, self.parents.data_ptr())
-        if c["op"] == "tree":
+                binding.dbt_kv_reserve(self.kv, at[b], half[b] * PAGE)
+        for b in reversed(range(B)):
+            binding.dbt_kv_reserve(self.kv, at[b], total[b])
+        if not keep:
+            self.tree = binding.make_tree(self.nodes, self.parents.data_ptr())
             self.tree_workspace = torch.empty(binding.dbt_tree_workspace_bytes(cfg, sum(self.nodes)), dtype=torch.uint8,
                                               device="cuda")
-        else:
-            # the nodes that a pass drops are grown again before the next one
-            kept = _kept(c)
-            self.paths = binding.make_paths(kept)
-            self.tree = binding.make_tree(self.nodes)
-            self.grow = binding.make_tree([n - len(p) for n, p in zip(self.nodes, kept)])
-            for b in range(c["batch"]):
-                binding.dbt_kv_truncate(self.kv, b, self.lens[b] + len(kept[b]))
+            return
+        kept = _kept(c)
+        self.tree = binding.make_tree(self.nodes[::-1])
+        self.paths = binding.make_paths(kept[::-1])
+        now = [n + len(p) for n, p in zip(self.lens, kept)]
+        for b in range(B):
+            binding.dbt_kv_truncate(self.kv, at[b], now[b])
+        # calls that grow the dropped nodes again, their pages in ascending order
+        # (one call, unless sequences are so short that they drop most of their pages)
+        table = self.table.tolist()
+        lost = sorted((table[b][j], at[b], b, j) for b in range(B) for j in range((now[b] + PAGE - 1) // PAGE, pages[b]))
+        last, self.grow, grown = -1, [], [0] * B
+        for b in range(B):
+            if pages[b] == (now[b] + PAGE - 1) // PAGE:
+                grown[at[b]], now[b] = total[b] - now[b], total[b]
+        for _, a, b, j in lost:
+            if a < last:
+                self.grow.append(binding.make_tree(grown))
+                grown = [0] * B
+            last, end = a, min(total[b], (j + 1) * PAGE)
+            grown[a] += end - now[b]
+            now[b] = end
+        self.grow.append(binding.make_tree(grown))
 
     def __del__(self):
         if getattr(self, "kv", None):
@@ -298,7 +318,8 @@ def run(s):
                                      s.tree_workspace.data_ptr(), stream)
             return s.out
         if op == "keep":
-            s.lib.dbt_tree_reserve(s.kv, s.grow)
+            for tree in s.grow:
+                s.lib.dbt_tree_reserve(s.kv, tree)
             s.lib.dbt_kv_keep(s.kv, s.tree, s.paths, stream)
             return {"k": s.k, "v": s.v}
         s.lib.dbt_sample(s.input, s.token.data_ptr(), s.prob.data_ptr(), s.workspace.data_ptr(), stream)
