@@ -36,9 +36,9 @@
 // bits: fused operations are the ones written here, no others.
 #pragma clang fp contract(off)
 
+namespace dbt {
 namespace {
 
-using namespace dbt;
 typedef unsigned long long u64;
 
 constexpr int kTile = 2048;         // tokens of one statistics tile
@@ -1038,6 +1038,9 @@ template <int NP> hipError_t launch(const Args &a, const dbt_sampling *p, bool c
 }
 
 }  // namespace
+}  // namespace dbt
+
+using namespace dbt;
 
 extern "C" size_t dbt_sample_workspace_bytes(int32_t rows, int32_t vocab) {
   if (rows < 1 || rows > 65535 || vocab < 1 || vocab > kMaxVocab) {
