@@ -524,18 +524,29 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_tree_keep(KeepSeqs s, KVRef kv, size_t layer_elems) {
   constexpr int EP = 16 / sizeof(T);
   __shared__ __attribute__((aligned(16))) T ks[kTreeNodes * 128], vs[kTreeNodes * 128];
+  __shared__ size_t block[2 * kTreeNodes];
+  __shared__ int slot[2 * kTreeNodes];
   const int g = blockIdx.x, i = blockIdx.z, t = threadIdx.x, DH = kv.d_h, pr = DH / EP;
   const int j0 = s.first[i], n = s.count[i] - j0, base = s.base[i];
-  const int *ptab = kv.page_table + (size_t)s.seq[i] * kv.mpps;
   T *k = (T *)kv.k + blockIdx.y * layer_elems, *v = (T *)kv.v + blockIdx.y * layer_elems;
-  auto krow = [&](int pos) { return k + (((size_t)ptab[pos >> 4] * kv.n_kv + g) * 16 + (pos & 15)) * DH; };
-  auto vcol = [&](int pos) { return v + ((size_t)ptab[pos >> 4] * kv.n_kv + g) * DH * 16 + (pos & 15); };
-  for (int e = t; e < n * pr; e += 256)
-    ((u32x4 *)ks)[e] = ((const u32x4 *)krow(base + s.path[i][j0 + e / pr]))[e % pr];
-  for (int e = t; e < n * DH; e += 256) vs[e] = vcol(base + s.path[i][j0 + e % n])[(e / n) * 16];
+  if (t < 2 * n) {  // the nodes' places: old ones, then new ones
+    const int j = t < n ? t : t - n, pos = base + (t < n ? s.path[i][j0 + j] : j0 + j);
+    const int page = kv.page_table[(size_t)s.seq[i] * kv.mpps + (pos >> 4)];
+    block[t] = ((size_t)page * kv.n_kv + g) * 16 * DH;
+    slot[t] = pos & 15;
+  }
   __syncthreads();
-  for (int e = t; e < n * pr; e += 256) ((u32x4 *)krow(base + j0 + e / pr))[e % pr] = ((const u32x4 *)ks)[e];
-  for (int e = t; e < n * DH; e += 256) vcol(base + j0 + e % n)[(e / n) * 16] = vs[e];
+  auto krow = [&](int j) { return (u32x4 *)(k + block[j] + slot[j] * DH); };
+  auto vcol = [&](int j) { return v + block[j] + slot[j]; };
+#pragma unroll 4
+  for (int e = t; e < n * pr; e += 256) ((u32x4 *)ks)[e] = krow(e / pr)[e % pr];
+#pragma unroll 4
+  for (int e = t; e < n * DH; e += 256) vs[e] = vcol(e % n)[(e / n) * 16];
+  __syncthreads();
+#pragma unroll 4
+  for (int e = t; e < n * pr; e += 256) krow(n + e / pr)[e % pr] = ((const u32x4 *)ks)[e];
+#pragma unroll 4
+  for (int e = t; e < n * DH; e += 256) vcol(n + e % n)[(e / n) * 16] = vs[e];
 }
 
 }  // namespace
