@@ -310,7 +310,7 @@ dbt_status dbt_tree_reserve(dbt_kv *kv, const dbt_tree *tree);
  * positions of sequence b are its nodes, their keys and values already there
  * (dbt_kv_fill); node i sees every position before them, itself and its
  * ancestors.  q and out, in the model's dtype: [n_paths][sum h_nodes][n_q][d_h],
- * paths 1..1 + n_branches as in a step (Eqs. (9), (12)).  The keys and values
+ * paths 1..1 + n_branches as in a step (Eqs. (9), (12)); out may be q itself.  The keys and values
  * that a node does not see leave no trace in its rows, whatever they hold.  The
  * same call repeats its bits; the number of splits of a long cache follows from
  * the whole call, so rows can differ by rounding from one batch to another. */
@@ -328,10 +328,10 @@ dbt_status dbt_decode_tree(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, cons
  * answered), the path follows the first child whose drafted token is the one
  * drawn after the node, as long as there is one.  Every array is host memory and
  * laid out as dbt_tree: h_tokens are the nodes' own tokens, h_drawn the tokens
- * drawn after them.  h_path
- * (room for sum h_nodes) receives the kept nodes' indices, ascending, sequence after sequence;
- * h_kept[b] is their number, h_next[b] (may be NULL) the token drawn after the last of
- * them (-1 for a sequence without nodes). */
+ * drawn after them.  h_path (room for sum h_nodes) receives the kept nodes'
+ * indices, ascending, sequence after sequence; h_kept[b] is their number,
+ * h_next[b] (may be NULL) the token drawn after the last of them (-1 for a
+ * sequence without nodes). */
 dbt_status dbt_tree_accept(int32_t batch, const int32_t *h_nodes, const int32_t *h_parents, const int32_t *h_tokens,
                            const int32_t *h_drawn, int32_t *h_path, int32_t *h_kept, int32_t *h_next);
 
@@ -363,6 +363,8 @@ typedef struct {
   int32_t n_branches;    /* 0..3; 0: the primary's distribution alone */
 } dbt_sample_in;
 
+/* Bytes of the workspace (256-byte aligned) of a dbt_sample of this size (0 on
+ * bad arguments).  Calls that may overlap need workspaces of their own. */
 size_t dbt_sample_workspace_bytes(int32_t rows, int32_t vocab);
 
 /* One token per row from the mixture m = alpha p + (1 - alpha) q of the readout

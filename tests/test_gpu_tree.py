@@ -160,6 +160,23 @@ def test_cache_beyond_one_splits_page_ids(dtype, nq, nkv, dh):
     c.sess.close()
 
 
+@pytest.mark.parametrize("dtype,nq,nkv,dh,branches,paths,long", [("bf16", 16, 4, 128, 3, 4, 6000), ("bf16", 8, 2, 128, 1, 1, 3333),
+                                                                 ("f32", 16, 4, 16, 3, 4, 2500)])
+def test_runs_over_many_short_sequences(dtype, nq, nkv, dh, branches, paths, long):
+    """More (sequence, KV head) pairs than workgroups, one of them long: runs of
+    pages begin and end inside sequences and go over several."""
+    rng = np.random.default_rng(11)
+    n = 40 if paths > 1 else 300
+    nodes = [64] + [int(x) for x in rng.integers(1, 4, n)]
+    lens = [long] + [int(x) for x in rng.integers(0, 300, n)]
+    order = rng.permutation(n + 1)
+    nodes, lens = [nodes[i] for i in order], [lens[i] for i in order]
+    c = Cache(dtype, nq, nkv, dh, [a + b for a, b in zip(lens, nodes)], branches=branches)
+    c.fill()
+    check(c, nodes, [p for m in nodes for p in random_tree(rng, m)], paths)
+    c.sess.close()
+
+
 @pytest.mark.parametrize("paths,nodes", [(4, [64, 50]), (1, [4, 1])])
 def test_more_than_1024_pages_in_one_workgroup(paths, nodes):
     """A sequence so long that the sixteen workgroups it is cut for have more
@@ -248,6 +265,25 @@ def test_what_a_node_does_not_see_leaves_no_trace(dtype, nq, nkv, dh, base, bad)
         c.fill()
         got = c.attend([n], up, q)
         assert not torch.isfinite(got[..., 5]).any() and torch.equal(got[..., :5], clean[..., :5])
+    c.sess.close()
+
+
+@pytest.mark.parametrize("dtype,dh,base", [("bf16", 128, 90), ("bf16", 128, 6000), ("f32", 20, 700)])
+def test_outputs_in_place_of_the_queries(dtype, dh, base):
+    rng = np.random.default_rng(2)
+    nodes = [30, 41, 3]
+    c = Cache(dtype, 8, 2, dh, [base + 30, 17 + 41, 300 + 3])
+    c.fill()
+    parents = [p for n in nodes for p in random_tree(rng, n)]
+    q = torch.randn((2, 74, 8, dh), generator=torch.Generator().manual_seed(5)).to(c.tt)
+    want = c.attend(nodes, parents, q)
+    up, qd = torch.tensor(parents, dtype=torch.int32, device="cuda"), q.cuda()
+    ws = torch.empty(c.B.dbt_tree_workspace_bytes(c.sess.cfg, 74), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    c.B.dbt_tree_attention(c.sess.kv, 0, c.B.make_tree(nodes, up.data_ptr()), 2, qd.data_ptr(), qd.data_ptr(),
+                           ws.data_ptr(), c.sess.stream)
+    torch.cuda.synchronize()
+    assert torch.equal(qd.cpu(), want)
     c.sess.close()
 
 
