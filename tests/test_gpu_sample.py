@@ -107,6 +107,16 @@ def test_rows_and_large_vocabularies(R, V, nb):
             check(z1, zb, alpha, rng.random(R).astype(np.float32), [k])
 
 
+@pytest.mark.parametrize("R,V,nb", [(2100, 5000, 1), (700, 9000, 0), (520, 16385, 0)])
+def test_parts_of_several_tiles_and_many_requests(R, V, nb):
+    """Rows enough to fill the chip (parts of two to four tiles), over 2048 of
+    them, over 96 different parameters."""
+    rng = np.random.default_rng(R)
+    z1, zb, alpha = logits(rng, R, V, nb)
+    kinds = KINDS + [(0.5 + 0.01 * i, 5 + i, 0.8, 0.0) for i in range(150)]
+    check(z1, zb, alpha, rng.random(R).astype(np.float32), [kinds[int(i)] for i in rng.integers(0, len(kinds), R)])
+
+
 @pytest.mark.parametrize("V", [5, 3000, 40000])
 @pytest.mark.parametrize("nb", [0, 1])
 def test_ties(V, nb):
