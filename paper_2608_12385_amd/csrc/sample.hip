@@ -18,12 +18,13 @@
 // that part alone again.
 //
 // Six kernels, for 64 rows of 128256 tokens with one branch and requests of every
-// kind: statistics of the tiles 21 us, row constants 9, weights and histograms 33,
-// cut classes 7, list 6, cut and draw 23 (a launch whose rows have no cut skips
-// the list and the cut classes); 500 rows of 50257 without branches: 20, 5, 40,
-// 6, 17, 20.  The floor is the logits read once, 13 and 20 us.  The weights are
+// kind: statistics of the tiles 21 us, row constants 9 (without branches the
+// weights' kernel finds the maximum itself), weights and histograms 33, cut
+// classes 7, list 6, cut and draw 23 (a call whose rows have no cut skips the list
+// and the cut classes); 500 rows of 50257 without branches: 16-20, none, 41, 6, 17, 20.
+// The floor is the logits read once, 13 and 20 us.  The weights are
 // bound by vector instructions, some 44 a token of which half are float64 (28 of
-// the 40 us); the statistics by memory without branches and by the exponentials
+// the 41 us); the statistics by memory without branches and by the exponentials
 // with one; the list by the lines of logits around its tokens; the row kernels by
 // their chains of dependent steps, a workgroup a row.
 #include <cmath>
@@ -62,7 +63,7 @@ struct ParamBlock {  // (kernel arguments: below 4 KB)
 };
 
 struct RowState {
-  double scale[4];  // m / max m = sum_j scale[j] exp(z_j - zmax[j])
+  double scale[4];  // several paths: m / max m = sum_j scale[j] exp(z_j - zmax[j])
   double inv_t;
   u64 least;        // weights below stay out (min-p; 1: nothing but zeros)
   u64 k_mass;       // mass of the classes before kc
@@ -318,8 +319,8 @@ __global__ __launch_bounds__(256) void k_sample_stats(Args a, ParamBlock pb, int
   }
 }
 
-// Row constants: every path's maximum and normaliser, and the largest mixture
-// value.  A tile holds none above ub = sum_j scale_j exp(max_j - zmax_j), while
+// Row constants of several paths: each one's maximum and normaliser, and the
+// largest mixture value.  A tile holds none above ub = sum_j scale_j exp(max_j - zmax_j), while
 // the token of a tile's maximum proves lb = max_j of the terms: only tiles with
 // ub >= lb (less a margin over both sides' rounding) are evaluated.
 template <int NP>
@@ -341,26 +342,22 @@ __global__ __launch_bounds__(kFinal) void k_sample_rows(Args a) {
   block_reduce_d<true>(M, red);
 #pragma unroll
   for (int j = 0; j < NP; ++j) {
-    // (one path: the sums only say whether the row is sound)
-    term[j] = NP > 1 && t < a.tiles ? pow2((st[j].x - M[j]) * kLog2eD) : 0.0;
-    S[j] = NP > 1 && st[j].y > 0.0 ? st[j].y * term[j] : st[j].y;
+    term[j] = t < a.tiles ? pow2((st[j].x - M[j]) * kLog2eD) : 0.0;
+    S[j] = st[j].y > 0.0 ? st[j].y * term[j] : st[j].y;
   }
   block_reduce_d<false>(S, red);
 #pragma unroll
   for (int j = 0; j < NP; ++j) ok = ok && M[j] > -INFINITY && S[j] == S[j];
   RowState rs;
-  rs.scale[0] = 1.0;
-  if (NP > 1) {
-    const double al = a.alpha[row];
-    ok = ok && al >= 0.0 && al <= 1.0;
-    rs.scale[0] = al / S[0];
+  const double al = a.alpha[row];
+  ok = ok && al >= 0.0 && al <= 1.0;
+  rs.scale[0] = al / S[0];
 #pragma unroll
-    for (int j = 1; j < NP; ++j) rs.scale[j] = (1.0 - al) / (NP - 1) / S[j];
-  }
+  for (int j = 1; j < NP; ++j) rs.scale[j] = (1.0 - al) / (NP - 1) / S[j];
 #pragma unroll
   for (int j = 0; j < NP; ++j) rs.zmax[j] = (float)M[j];
   double mmax = 1.0;
-  if (NP > 1 && ok) {
+  if (ok) {
     double lb[1] = {0.0}, ub = 0.0;
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
@@ -405,12 +402,31 @@ __global__ __launch_bounds__(256) void k_sample_weigh(Args a) {
   __shared__ u64 mass[kClasses];
   __shared__ unsigned count[kClasses];
   const int part = blockIdx.x, row = blockIdx.y, t = threadIdx.x;
-  const RowState r = a.w.state[row];
-  if (!r.valid) return;
+  RowState r = a.w.state[row];
   const int lo = part * a.part, hi = min(a.V, lo + a.part);
   mass[t] = 0;
   count[t] = 0;
-  __syncthreads();
+  if constexpr (NP == 1) {
+    // the path's maximum straight from the tiles' statistics (+infinity: the row has no answer)
+    __shared__ float top[4];
+    float m = -INFINITY;
+    for (int i = t; i < a.tiles; i += 256) {
+      const double2 st = a.w.stats[((size_t)row * a.tiles + i) * 4];
+      m = st.y == st.y ? fmaxf(m, (float)st.x) : INFINITY;
+    }
+    m = wave_max_dpp(m);
+    if ((t & 63) == 0) top[t >> 6] = m;
+    __syncthreads();
+    r.zmax[0] = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    r.valid = r.zmax[0] > -INFINITY && r.zmax[0] < INFINITY;
+    if (part == 0 && t == 0) {
+      a.w.state[row].zmax[0] = r.zmax[0];
+      a.w.state[row].valid = r.valid;
+    }
+  } else {
+    __syncthreads();
+  }
+  if (!r.valid) return;
   u64 kept = 0;  // no cut: kept mass; cut: mass of the low class
   unsigned low = 0;
   // four neighbours a thread (their classes are one store), the next round's
@@ -1023,8 +1039,10 @@ template <int NP> hipError_t launch(const Args &a, const dbt_sampling *p, bool c
     if (const hipError_t e = hipGetLastError()) return e;
     r0 += n;
   }
-  hipLaunchKernelGGL(k_sample_rows<NP>, dim3(a.rows), dim3(kFinal), 0, st, a);
-  if (const hipError_t e = hipGetLastError()) return e;
+  if constexpr (NP > 1) {
+    hipLaunchKernelGGL(k_sample_rows<NP>, dim3(a.rows), dim3(kFinal), 0, st, a);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
   hipLaunchKernelGGL(k_sample_weigh<NP>, dim3(a.parts, a.rows), dim3(256), 0, st, a);
   if (const hipError_t e = hipGetLastError()) return e;
   if (cuts) {
