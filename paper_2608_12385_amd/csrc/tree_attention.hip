@@ -223,11 +223,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     float m_run[RT];
     floatx4 acc[RT][8], acc_l[RT];  // acc_l: the sums of the rounded probabilities, by one more value multiply with V = 1
     const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-  #pragma unroll
+#pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       m_run[rt] = kNoScore;
       acc_l[rt] = floatx4{0.f, 0.f, 0.f, 0.f};
-  #pragma unroll
+#pragma unroll
       for (int c = 0; c < 8; ++c) acc[rt][c] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
     const int kpage = r >> 3, kpos = 8 * ((r >> 2) & 1) + (r & 3);
@@ -238,16 +238,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     auto pair = [&](int pg0, const uint16_t *kb, const uint16_t *vb, auto masked) __attribute__((always_inline)) {
       constexpr bool MASKED = decltype(masked)::value;
       u32x4 ka[4], kc[4], vf[8];
-  #pragma unroll
+#pragma unroll
       for (int s = 0; s < 4; ++s) {
         ka[s] = *(const u32x4 *)&kb[(kpage * 16 + kpos) * DH + ((s * 4 + gq) ^ kswz(kpos)) * 8];
         kc[s] = *(const u32x4 *)&kb[(kpage * 16 + kpos + 4) * DH + ((s * 4 + gq) ^ kswz(kpos + 4)) * 8];
       }
       floatx4 sc[RT][2];
-  #pragma unroll
+#pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         sc[rt][0] = sc[rt][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-  #pragma unroll
+#pragma unroll
         for (int s = 0; s < 4; ++s) {
           sc[rt][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka[s]),
                                                               __builtin_bit_cast(bf16x8, qf[rt][s]), sc[rt][0], 0, 0, 0);
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                                                               __builtin_bit_cast(bf16x8, qf[rt][s]), sc[rt][1], 0, 0, 0);
         }
       }
-  #pragma unroll
+#pragma unroll
       for (int c = 0; c < 8; ++c) vf[c] = *(const u32x4 *)&vb[(vpage * DH + c * 16 + r) * 16 + vpos];
       const int kp0 = (pb + pg0 + vpage) * 16 + vpos;  // position of this lane's first score
       const bool page_ok = pg0 + vpage < npg;
@@ -288,9 +288,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       // for its chain of maximum, exponentials and conversion)
       float s[RT][8], m_new[RT];
       bool grow = false;
-  #pragma unroll
+#pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-  #pragma unroll
+#pragma unroll
         for (int e = 0; e < 4; ++e) {
           s[rt][e] = sc[rt][0][e];
           s[rt][4 + e] = sc[rt][1][e];
@@ -302,12 +302,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                                 : rel >= 0            ? (uint32_t)(line >> rel) & 0xff
                                 : rel > -8            ? (uint32_t)((line << -rel) | ((1u << -rel) - 1)) & 0xff
                                                       : 0xffu;
-  #pragma unroll
+#pragma unroll
           for (int e = 0; e < 8; ++e)
             if (!((seen >> e) & 1)) s[rt][e] = -INFINITY;
         }
         float mt = s[rt][0];
-  #pragma unroll
+#pragma unroll
         for (int e = 1; e < 8; ++e) mt = fmaxf(mt, s[rt][e]);
         // lazy rescaling: a row's base moves only when the pair's maximum exceeds it
         // by more than kLazyMargin, so exponentials stay <= 2^kLazyMargin
@@ -317,29 +317,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         grow |= up;
       }
       if (__any(grow)) {  // (a factor of exactly 1 where the base stays)
-  #pragma unroll
+#pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
           const float corr = __builtin_amdgcn_exp2f(m_run[rt] - m_new[rt]);
           acc_l[rt] = acc_l[rt] * corr;
-  #pragma unroll
+#pragma unroll
           for (int c = 0; c < 8; ++c) acc[rt][c] = acc[rt][c] * corr;
           m_run[rt] = m_new[rt];
         }
       }
       u32x4 pf[RT];
-  #pragma unroll
+#pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         float p[8];
-  #pragma unroll
+#pragma unroll
         for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][e], scale, -m_new[rt]));
         // (probabilities are rounded to bf16 for the matrix unit; their sum is of the rounded ones)
         pf[rt] = u32x4{pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7])};
       }
-  #pragma unroll
+#pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         acc_l[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones),
                                                             __builtin_bit_cast(bf16x8, pf[rt]), acc_l[rt], 0, 0, 0);
-  #pragma unroll
+#pragma unroll
         for (int c = 0; c < 8; ++c)
           acc[rt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[c]),
                                                                __builtin_bit_cast(bf16x8, pf[rt]), acc[rt][c], 0, 0, 0);
@@ -393,12 +393,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       // whatever their weights
       for (int pos = max(base, pages0 * 16); pos < min(len, pages1 * 16); ++pos) {
         const uint16_t *v = vbase + ((size_t)ptab[pos >> 4] * n_kv + g) * PB + (pos & 15);
-  #pragma unroll
+#pragma unroll
         for (int c = 0; c < 8; ++c)
-  #pragma unroll
+#pragma unroll
           for (int d = 0; d < 4; ++d) {
             const uint16_t x = v[(16 * c + 4 * gq + d) * 16];
-  #pragma unroll
+#pragma unroll
             for (int rt = 0; rt < RT; ++rt)
               if ((x & 0x7f80) == 0x7f80 && ((line_s[node[rt]] >> (pos - base)) & 1)) acc[rt][c][d] += bf2f(x);
           }
@@ -411,12 +411,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       if (pc.is_whole()) {
         const float inv = 1.f / acc_l[rt][0];
         uint16_t *o = (uint16_t *)a.O + place(rho) * DH + 4 * gq;
-  #pragma unroll
+#pragma unroll
         for (int c = 0; c < 8; ++c)
           *(u32x2 *)(o + 16 * c) = u32x2{pack2(acc[rt][c][0] * inv, acc[rt][c][1] * inv), pack2(acc[rt][c][2] * inv, acc[rt][c][3] * inv)};
       } else {
         const size_t to = ((size_t)pc.slot(w) * a.blocks + blk) * a.block + rho - row0;
-  #pragma unroll
+#pragma unroll
         for (int c = 0; c < 8; ++c)
           *(float4 *)(a.opart + to * DH + 16 * c + 4 * gq) = make_float4(acc[rt][c][0], acc[rt][c][1], acc[rt][c][2], acc[rt][c][3]);
         if (gq == 0) *(float2 *)(a.ostat + to * 2) = make_float2(m_run[rt], acc_l[rt][0]);
