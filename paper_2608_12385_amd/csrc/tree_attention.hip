@@ -121,21 +121,25 @@ constexpr float kLazyMargin = 8.f;
 // running maximum and sum a row.  Rows see different keys only in pages from
 // position `base` on; those pairs take a masked path.
 //
-// Up to 64 rows RT is 1, so that all four SIMDs have a part of them (32 x 4096
-// positions, eight KV heads: 97 us with 8 rows and 111 with 64; with RT = 2 two
-// SIMDs stand idle, 100 and 115); more rows are faster with two tiles a wave, whose
-// softmax steps run side by side and which read LDS half as often.  Eight
-// waves that also share a stage's pairs (merged at the end) take 107 us for those 64
-// rows but 142 against 111 for 48 x 200-4000, since nothing runs while the
-// compute unit's one workgroup begins its next piece.
+// Up to 64 rows RT is 1, so that all four SIMDs have a part of them, and one
+// workgroup alone reads each page: the loads' non-temporal hint takes 97 us to 90
+// with 8 rows (32 x 4096 positions, eight KV heads) and 111 to 104 with 64.  More
+// rows are faster with two tiles a wave, whose softmax steps run side by side and
+// which read LDS half as often; the hint gains nothing there, and where several blocks
+// share the pages in an L2 it costs 2-5 %.  Without the hint 8 and 64 rows take 100
+// and 115 us with RT = 2, which leaves two SIMDs idle; eight waves that also share a
+// stage's pairs (merged at the end) take 107 for the 64 rows but 142 against 111 for
+// 48 x 200-4000, since nothing runs while the compute unit's one workgroup begins
+// its next piece.
 //
-// Bound: up to 64 rows the memory (97 us: 5.6 TB/s).  From 128 rows the matrix
+// Bound: up to 64 rows the memory (90 us: 6.1 TB/s).  From 128 rows the matrix
 // unit beside the softmax: 16 x 300-1500 with 1024 rows 54 us, 3.1e10 operations
 // (the longest sequence alone takes 45); 8 x 16k-32k with 256 rows 285 us, 2.1e11
 // operations, 215 without the loads and 171 without the multiplies.
 template <int RT, typename QT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_tree_attn_bf16(TreeAttn a) {
   constexpr int DH = 128, NW = 4, SP = 4, PB = 16 * DH;  // waves; pages of a stage; elements of a page
+  constexpr int kOnce = RT == 1 ? 2 : 0;  // the loads' non-temporal hint
   static_assert(SP == NW && kTreeStagePages % SP == 0, "a page per wave, whole stages");
   // two sets of stage buffers, separate arrays so that the loads filling one
   // set are told apart from the reads of the other
@@ -173,12 +177,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       for (int j = 0; j < 4; ++j) {
         const int row = 4 * j + (lane >> 4);
         __builtin_amdgcn_global_load_lds((const void *)(kbase + at + row * DH + ((lane & 15) ^ kswz(row)) * 8),
-                                         (lds_void *)(kb + wave * PB + 4 * j * DH), 16, 0, 0);
+                                         (lds_void *)(kb + wave * PB + 4 * j * DH), 16, 0, kOnce);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         __builtin_amdgcn_global_load_lds((const void *)(vbase + at + 32 * j * 16 + lane * 8),
-                                         (lds_void *)(vb + wave * PB + 32 * j * 16), 16, 0, 0);
+                                         (lds_void *)(vb + wave * PB + 32 * j * 16), 16, 0, kOnce);
     };
     auto next = [&](int st, uint16_t *kb, uint16_t *vb) __attribute__((always_inline)) {
       dma(pid_s[min(st * SP + wave, npg - 1)], kb, vb);
