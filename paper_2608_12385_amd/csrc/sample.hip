@@ -276,47 +276,42 @@ __device__ __forceinline__ void set_params(const Args &a, const RowParams &p, in
   r.listed = 0;
 }
 
-// Statistics of a tile by one wave: each path's maximum and, with several
-// paths, the sum of exponentials; NaN for a tile that holds a NaN or +infinity.
-// Each lane has its 32 values of a path in flight together.
-template <int NP>
+// Statistics of a tile of path blockIdx.z by one wave: its maximum and, with
+// several paths (SUM), the sum of exponentials; NaN for a tile that holds a NaN or
+// +infinity.  Each lane has its 32 values in flight together.
+template <bool SUM>
 __global__ __launch_bounds__(256) void k_sample_stats(Args a, ParamBlock pb, int row0) {
-  const int lane = threadIdx.x & 63, row = row0 + blockIdx.y;
+  const int lane = threadIdx.x & 63, row = row0 + blockIdx.y, j = blockIdx.z;
   const int tile = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (blockIdx.x == 0 && threadIdx.x == 0) set_params(a, pb.set[pb.of[blockIdx.y]], row);
+  if (blockIdx.x == 0 && j == 0 && threadIdx.x == 0) set_params(a, pb.set[pb.of[blockIdx.y]], row);
   if (tile >= a.tiles) return;
   constexpr int N = kTile / 64;
+  const float *z = path_row(a, j, row) + tile * kTile;
+  const int n = a.V - tile * kTile;
+  float v[N];
 #pragma unroll
-  for (int j = 0; j < NP; ++j) {
-    const float *z = path_row(a, j, row) + tile * kTile;
-    const int n = a.V - tile * kTile;
-    float v[N];
+  for (int k = 0; k < N; ++k) v[k] = z[min(k * 64 + lane, n - 1)];
+  float mx = -INFINITY;
+  bool bad = false;
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = z[min(k * 64 + lane, n - 1)];
-    float mx = -INFINITY;
-    bool bad = false;
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      mx = fmaxf(mx, v[k]);
-      bad |= !(v[k] < INFINITY);
-    }
-    mx = wave_max_dpp(mx);
-    double sum = 0.0;
-    if (NP > 1 && mx > -INFINITY) {
+  for (int k = 0; k < N; ++k) {
+    mx = fmaxf(mx, v[k]);
+    bad |= !(v[k] < INFINITY);
+  }
+  mx = wave_max_dpp(mx);
+  double sum[1] = {0.0};
+  if constexpr (SUM) {
+    if (mx > -INFINITY) {
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         const double e = pow2(((double)v[k] - (double)mx) * kLog2eD);
-        sum += k * 64 + lane < n ? e : 0.0;  // (values past the row repeat its last)
+        sum[0] += k * 64 + lane < n ? e : 0.0;  // (values past the row repeat its last)
       }
     }
-    if (NP > 1) {
-      double one[1] = {sum};
-      wave_reduce_d<false>(one);
-      sum = one[0];
-    }
-    if (__any(bad)) sum = __longlong_as_double(0x7ff8000000000000ll);
-    if (lane == 63) a.w.stats[((size_t)row * a.tiles + tile) * 4 + j] = make_double2(mx, sum);
+    wave_reduce_d<false>(sum);
   }
+  if (__any(bad)) sum[0] = __longlong_as_double(0x7ff8000000000000ll);
+  if (lane == 63) a.w.stats[((size_t)row * a.tiles + tile) * 4 + j] = make_double2(mx, sum[0]);
 }
 
 // Row constants of several paths: each one's maximum and normaliser, and the
@@ -1035,7 +1030,7 @@ template <int NP> hipError_t launch(const Args &a, const dbt_sampling *p, bool c
       if (k == sets) pb.set[sets++] = RowParams{q.temperature, q.top_p, q.min_p, q.top_k};
       pb.of[n] = (uint8_t)(last = k);
     }
-    hipLaunchKernelGGL(k_sample_stats<NP>, dim3((a.tiles + 3) / 4, n), dim3(256), 0, st, a, pb, r0);
+    hipLaunchKernelGGL(k_sample_stats<(NP > 1)>, dim3((a.tiles + 3) / 4, n, NP), dim3(256), 0, st, a, pb, r0);
     if (const hipError_t e = hipGetLastError()) return e;
     r0 += n;
   }
