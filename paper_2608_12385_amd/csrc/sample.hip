@@ -365,17 +365,22 @@ __global__ __launch_bounds__(kFinal) void k_sample_rows(Args a) {
     if (t < a.tiles && ub >= lb[0] * (1.0 - 1e-9)) list[atomicAdd(&nlist, 1)] = t;  // (a maximum has no order)
     __syncthreads();
     double mx[1] = {0.0};
-    // two tiles at a time, their loads in flight together (a last one twice)
-    constexpr int N = kTile / kFinal;
-    for (int n = 0; n < nlist; n += 2) {
-      float z[2 * N][NP];
+    // G tiles at a time, their loads in flight together (a last one again)
+    constexpr int N = kTile / kFinal, G = 4;
+    const int tiles = __builtin_amdgcn_readfirstlane(nlist);
+    for (int n = 0; n < tiles; n += G) {
+      float z[G * N][NP];
 #pragma unroll
-      for (int k = 0; k < 2 * N; ++k)
+      for (int k = 0; k < G * N; ++k)
 #pragma unroll
         for (int j = 0; j < NP; ++j)
-          z[k][j] = path_row(a, j, row)[min(a.V - 1, list[min(n + k / N, nlist - 1)] * kTile + k % N * kFinal + t)];
+          z[k][j] = path_row(a, j, row)[min(a.V - 1, list[min(n + k / N, tiles - 1)] * kTile + k % N * kFinal + t)];
 #pragma unroll
-      for (int k = 0; k < 2 * N; ++k) mx[0] = fmax(mx[0], mixture<NP>(rs, z[k]));
+      for (int g = 0; g < G; ++g) {
+        if (n + g >= tiles) break;
+#pragma unroll
+        for (int k = g * N; k < g * N + N; ++k) mx[0] = fmax(mx[0], mixture<NP>(rs, z[k]));
+      }
     }
     block_reduce_d<true>(mx, red);
     mmax = mx[0];
