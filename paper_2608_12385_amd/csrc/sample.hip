@@ -18,8 +18,8 @@
 // that part alone again.
 //
 // Six kernels, for 64 rows of 128256 tokens with one branch and requests of every
-// kind: statistics of the tiles 21 us, row constants 9 (without branches the
-// weights' kernel finds the maximum itself), weights and histograms 33, cut
+// kind: statistics of the tiles 20 us, row constants 9 (without branches the
+// weights' kernel finds the maximum itself), weights and histograms 32, cut
 // classes 7, list 6, cut and draw 23 (a call whose rows have no cut skips the list
 // and the cut classes); 500 rows of 50257 without branches: 16-20, none, 41, 6, 17, 20.
 // The floor is the logits read once, 13 and 20 us.  The weights are
