@@ -188,6 +188,8 @@ class _Cache:
         self.parents = torch.cat(up).to(torch.int32).cuda()
         if own:
             self._open(layers, pages, half, total)
+            if c["op"] == "keep":
+                _grow_again(self, pages, half, total)
 
     def _open(self, layers, pages, half, total):
         from paper_2608_12385_amd import binding
@@ -210,49 +212,63 @@ class _Cache:
         self.page_table = torch.full((c["batch"], self.mpps), -1, dtype=torch.int32, device="cuda")
         self.kv = binding.dbt_kv_create(self.model, self.k.data_ptr(), self.v.data_ptr(), self.num_pages,
                                         self.page_table.data_ptr(), self.mpps)
-        # The library hands out the lowest free page first.  Sequences whose
-        # nodes are dropped and grown again stand in reverse, so that growing
-        # them in a row takes the pages of the table again.
-        B, keep = c["batch"], c["op"] == "keep"
-        at = [B - 1 - b if keep else b for b in range(B)]
-        for b in range(B):
+        for b in range(c["batch"]):
             if half[b]:
-                binding.dbt_kv_reserve(self.kv, at[b], half[b] * PAGE)
-        for b in reversed(range(B)):
-            binding.dbt_kv_reserve(self.kv, at[b], total[b])
-        if not keep:
-            self.tree = binding.make_tree(self.nodes, self.parents.data_ptr())
+                binding.dbt_kv_reserve(self.kv, b, half[b] * PAGE)
+        for b in reversed(range(c["batch"])):
+            binding.dbt_kv_reserve(self.kv, b, total[b])
+        self.tree = binding.make_tree(self.nodes, self.parents.data_ptr())
+        if c["op"] == "tree":
             self.tree_workspace = torch.empty(binding.dbt_tree_workspace_bytes(cfg, sum(self.nodes)), dtype=torch.uint8,
                                               device="cuda")
-            return
-        kept = _kept(c)
-        self.tree = binding.make_tree(self.nodes[::-1])
-        self.paths = binding.make_paths(kept[::-1])
-        now = [n + len(p) for n, p in zip(self.lens, kept)]
-        for b in range(B):
-            binding.dbt_kv_truncate(self.kv, at[b], now[b])
-        # calls that grow the dropped nodes again, their pages in ascending order
-        # (one call, unless sequences are so short that they drop most of their pages)
-        table = self.table.tolist()
-        lost = sorted((table[b][j], at[b], b, j) for b in range(B) for j in range((now[b] + PAGE - 1) // PAGE, pages[b]))
-        last, self.grow, grown = -1, [], [0] * B
-        for b in range(B):
-            if pages[b] == (now[b] + PAGE - 1) // PAGE:
-                grown[at[b]], now[b] = total[b] - now[b], total[b]
-        for _, a, b, j in lost:
-            if a < last:
-                self.grow.append(binding.make_tree(grown))
-                grown = [0] * B
-            last, end = a, min(total[b], (j + 1) * PAGE)
-            grown[a] += end - now[b]
-            now[b] = end
-        self.grow.append(binding.make_tree(grown))
+        else:
+            self.paths = binding.make_paths(_kept(c))
+            for b in range(c["batch"]):
+                binding.dbt_kv_truncate(self.kv, b, self.lens[b])
 
     def __del__(self):
         if getattr(self, "kv", None):
             self.lib.dbt_kv_destroy(self.kv)
         if getattr(self, "model", None):
             self.lib.dbt_destroy(self.model)
+
+
+def _grow_again(s, pages, half, total):
+    """Lets a pass over kept paths run again on the same cache: it grows the
+    nodes that the last one dropped, on the pages they had.  The library hands
+    out the lowest free page first, so the sequences stand in reverse, in which
+    order growing them takes the pages of the table again."""
+    B = s.c["batch"]
+    kept = _kept(s.c)
+    at = [B - 1 - b for b in range(B)]
+    for b in range(B):
+        s.lib.dbt_kv_truncate(s.kv, b, 0)
+    for b in range(B):
+        if half[b]:
+            s.lib.dbt_kv_reserve(s.kv, at[b], half[b] * PAGE)
+    for b in reversed(range(B)):
+        s.lib.dbt_kv_reserve(s.kv, at[b], total[b])
+    s.tree = s.lib.make_tree(s.nodes[::-1])
+    s.paths = s.lib.make_paths(kept[::-1])
+    now = [n + len(p) for n, p in zip(s.lens, kept)]
+    for b in range(B):
+        s.lib.dbt_kv_truncate(s.kv, at[b], now[b])
+    # one call, unless sequences are so short that they drop most of their pages:
+    # then calls whose pages are handed out in ascending order each
+    table = s.table.tolist()
+    lost = sorted((table[b][j], at[b], b, j) for b in range(B) for j in range((now[b] + PAGE - 1) // PAGE, pages[b]))
+    last, s.grow, grown = -1, [], [0] * B
+    for b in range(B):
+        if pages[b] == (now[b] + PAGE - 1) // PAGE:
+            grown[at[b]], now[b] = total[b] - now[b], total[b]
+    for _, a, b, j in lost:
+        if a < last:
+            s.grow.append(s.lib.make_tree(grown))
+            grown = [0] * B
+        last, end = a, min(total[b], (j + 1) * PAGE)
+        grown[a] += end - now[b]
+        now[b] = end
+    s.grow.append(s.lib.make_tree(grown))
 
 
 class _Tree(_Cache):
