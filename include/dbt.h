@@ -313,14 +313,16 @@ dbt_status dbt_tree_reserve(dbt_kv *kv, const dbt_tree *tree);
  * paths 1..1 + n_branches as in a step (Eqs. (9), (12)); out may be q itself.  The keys and values
  * that a node does not see leave no trace in its rows, whatever they hold.  The
  * same call repeats its bits; the number of splits of a long cache follows from
- * the whole call, so rows can differ by rounding from one batch to another. */
+ * the whole call (its sequences, nodes and paths), so rows can differ by rounding
+ * from one batch, or number of paths, to another. */
 dbt_status dbt_tree_attention(dbt_kv *kv, int32_t layer, const dbt_tree *tree, int32_t n_paths, const void *q,
                               void *out, void *workspace, dbt_stream stream);
 
 /* dbt_decode_step over the nodes of a tree: in->batch is sum h_nodes (at most
  * max_batch), its tokens or residual inputs and every output are per node, and
  * node i has position len_b + its depth.  The primary appends the nodes' keys and values, the
- * sequences grow by their nodes. */
+ * sequences grow by their nodes.  The primary's outputs, keys and values are the
+ * same bits with the branch on and off. */
 dbt_status dbt_decode_tree(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, const dbt_tree *tree, int32_t branch_on,
                            dbt_step_out *out, void *workspace, dbt_stream stream);
 

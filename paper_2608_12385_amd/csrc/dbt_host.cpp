@@ -1501,8 +1501,10 @@ void schedule_tree(const dbt_config &c, int block, int blocks, TreeSeqs *g) {
   for (int i = 0; i < g->n; ++i) g->first[i + 1] = g->first[i] + c.n_kv_heads * (g->whole ? 1 : (stages(i) + g->pad - 1) / g->pad * g->pad);
 }
 
-// base[b]: positions of sequence b before its nodes.
-TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths, const int *base, char *ws) {
+// base[b]: positions of sequence b before its nodes.  The units are cut as for
+// cut_paths >= n_paths paths: a step's cuts, whose merges round, must not depend
+// on the branch (fewer blocks of rows than they were made for fit the workspace).
+TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths, int cut_paths, const int *base, char *ws) {
   const dbt_config &cf = m->cfg;
   TreePlan p;
   p.parents = t->parents;
@@ -1512,9 +1514,14 @@ TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths
   p.opart = (float *)(ws + L.opart);
   p.ostat = (float *)(ws + L.ostat);
   for (int b = 0; b < t->batch; ++b) p.max_nodes = std::max(p.max_nodes, t->h_nodes[b]);
-  const int rows = p.max_nodes * n_paths * (cf.n_q_heads / cf.n_kv_heads);
-  p.block = tree_block_rows(rows, cf.dtype);
-  p.blocks = (rows + p.block - 1) / p.block;
+  auto blocks_of = [&](int paths, int *block, int *blocks) {
+    const int rows = p.max_nodes * paths * (cf.n_q_heads / cf.n_kv_heads);
+    *block = tree_block_rows(rows, cf.dtype);
+    *blocks = (rows + *block - 1) / *block;
+  };
+  blocks_of(n_paths, &p.block, &p.blocks);
+  int cut_block, cut_blocks;
+  blocks_of(cut_paths, &cut_block, &cut_blocks);
   int off = 0;
   for (int b = 0; b < t->batch; ++b) {
     const int n = t->h_nodes[b];
@@ -1530,7 +1537,7 @@ TreePlan plan_tree(const dbt_model *m, const dbt_tree *t, int nodes, int n_paths
     g.nodes[g.n++] = n;
     off += n;
   }
-  for (TreeSeqs &g : p.groups) schedule_tree(cf, p.block, p.blocks, &g);
+  for (TreeSeqs &g : p.groups) schedule_tree(cf, cut_block, cut_blocks, &g);
   return p;
 }
 
@@ -1907,7 +1914,7 @@ dbt_status dbt_tree_attention(dbt_kv *kv, int32_t layer, const dbt_tree *tree, i
     base[b] = kv->len[b] - tree->h_nodes[b];
     if (base[b] < 0) return fail(DBT_ERR_ARG, "sequence %d has %d positions and %d nodes", b, kv->len[b], tree->h_nodes[b]);
   }
-  const TreePlan plan = plan_tree(kv->m, tree, nodes, n_paths, base.data(), (char *)workspace);
+  const TreePlan plan = plan_tree(kv->m, tree, nodes, n_paths, n_paths, base.data(), (char *)workspace);
   hipStream_t st = (hipStream_t)stream;
   if ((s = flush(kv, nullptr, 0, st))) return s;
   TreeAttn a{};
@@ -1946,7 +1953,8 @@ dbt_status dbt_decode_tree(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, cons
   if ((s = check_tree_growth(kv, tree))) return s;
   const int nb = n_branches(cf), R = nodes, Rp = round16(nodes);
   const Rows rows{R, Rp, 0, on ? 1 + nb : 1};
-  const TreePlan plan = plan_tree(m, tree, nodes, cf.compute_matched ? 1 : rows.np, kv->len.data(), (char *)workspace);
+  const TreePlan plan = plan_tree(m, tree, nodes, cf.compute_matched ? 1 : rows.np, cf.compute_matched ? 1 : 1 + nb,
+                                  kv->len.data(), (char *)workspace);
   hipStream_t st = (hipStream_t)stream;
   if ((s = ensure_device(m, st))) return s;  // before any state changes
   m->bnd_kv = nullptr;
