@@ -341,7 +341,9 @@ dbt_status dbt_tree_accept(int32_t batch, const int32_t *h_nodes, const int32_t 
  * NULL) are nodes; h_kept[b] of them stay, those with the ascending indices in
  * h_path [sum h_kept], sequence after sequence.  Their keys and values move, in
  * every layer, to the first positions of the nodes; the sequence ends behind them and gives
- * back the pages past its end. */
+ * back the pages past its end.  Sequences go in order, 32 with moved nodes a launch: a
+ * call that fails in a later launch (DBT_ERR_HIP) has kept the paths of the first
+ * sequences, as their lengths say, and left the others as they were. */
 dbt_status dbt_kv_keep(dbt_kv *kv, const dbt_tree *tree, const int32_t *h_kept, const int32_t *h_path,
                        dbt_stream stream);
 

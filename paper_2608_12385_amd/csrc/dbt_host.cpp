@@ -2046,6 +2046,17 @@ dbt_status dbt_kv_keep(dbt_kv *kv, const dbt_tree *tree, const int32_t *h_kept, 
   }
   hipStream_t st = (hipStream_t)stream;
   if ((s = flush(kv, nullptr, 0, st))) return s;
+  // Sequences end at their paths once the launch that moves their nodes is
+  // enqueued: should a later launch fail, none is left between its two states.
+  int done = 0;
+  auto end_sequences = [&](int to) {
+    for (; done < to; ++done) {
+      const int len = kv->len[done] - tree->h_nodes[done] + h_kept[done];
+      give_back_pages(kv, done, (size_t)(len + kPage - 1) / kPage);
+      kv->len[done] = len;
+    }
+    if (kv->m->bnd_kv == kv) kv->m->bnd_kv = nullptr;
+  };
   KeepSeqs ks;
   ks.n = 0;
   const KVRef first = kv_layer(kv, 0);
@@ -2065,17 +2076,13 @@ dbt_status dbt_kv_keep(dbt_kv *kv, const dbt_tree *tree, const int32_t *h_kept, 
       if (ks.n == kKeepSeqs) {
         HIPCHK(launch_tree_keep(ks, first, cf.n_layers, layer_elems, cf.dtype, st));
         ks.n = 0;
+        end_sequences(b + 1);
       }
     }
     off += kept;
   }
   HIPCHK(launch_tree_keep(ks, first, cf.n_layers, layer_elems, cf.dtype, st));
-  for (int b = 0; b < tree->batch; ++b) {
-    const int len = kv->len[b] - tree->h_nodes[b] + h_kept[b];
-    give_back_pages(kv, b, (size_t)(len + kPage - 1) / kPage);
-    kv->len[b] = len;
-  }
-  if (kv->m->bnd_kv == kv) kv->m->bnd_kv = nullptr;
+  end_sequences(tree->batch);
   return DBT_OK;
 } catch (const std::exception &) {
   return fail(DBT_ERR_ARG, "out of host memory");
