@@ -1,5 +1,5 @@
 """Kept paths on the stand-in for the HIP runtime: a call of several launches that
-fails in between."""
+fails in between, and the pages that come back."""
 import ctypes
 import os
 import subprocess
@@ -9,7 +9,7 @@ import pytest
 
 from tests.test_launches_cpu import FAKE, ROOT, Program, fake  # noqa: F401
 
-HIP = 6
+NO_PAGES, HIP = 3, 6
 
 
 def run_child(fake, name):  # noqa: F811
@@ -19,7 +19,7 @@ def run_child(fake, name):  # noqa: F811
     assert r.returncode == 0 and "done" in r.stdout, (r.stdout + r.stderr)[-3000:]
 
 
-@pytest.mark.parametrize("name", ["launches"])
+@pytest.mark.parametrize("name", ["launches", "pages"])
 def test_kept_paths(fake, name):  # noqa: F811
     run_child(fake, name)
 
@@ -75,9 +75,31 @@ def launches(fk):
         assert held() == after
 
 
+def pages(fk):
+    """A pool of exactly the pages that the sequences hold: what a keep gives back,
+    and no page more, can be taken again."""
+    p = Program("f32", max_batch=4)
+    B = p.B
+    kv, _table = p.cache(pages=9, nseq=4)
+    fk.fake_reset(-1)
+    for b, n in enumerate((40, 33, 48)):
+        B.dbt_kv_reserve(kv, b, n)
+    assert p.status(B.dbt_kv_reserve, kv, 3, 1) == NO_PAGES
+    held = [B.dbt_kv_pages(kv, b) for b in range(3)]
+    t = B.make_tree([30, 2, 40])  # positions 10, 31 and 8 before the nodes
+    assert p.status(B.dbt_kv_keep, kv, t, B.make_paths([[0, 4, 20], [1], []]), 0) == 0
+    assert [B.dbt_kv_length(kv, b) for b in range(3)] == [13, 32, 8]
+    assert [B.dbt_kv_pages(kv, b) for b in range(3)] == [held[0][:1], held[1][:2], held[2][:1]]
+    back = sorted(held[0][1:] + held[1][2:] + held[2][1:])
+    assert len(back) == 5
+    assert p.status(B.dbt_kv_reserve, kv, 3, 6 * 16) == NO_PAGES
+    assert B.dbt_kv_reserve(kv, 3, 5 * 16) == back
+    assert p.status(B.dbt_kv_reserve, kv, 3, 5 * 16 + 1) == NO_PAGES
+
+
 if __name__ == "__main__":
     sys.path.insert(0, ROOT)
     fk = ctypes.CDLL(sys.argv[2])
     fk.fake_kernel.restype = ctypes.c_char_p
-    {"launches": launches}[sys.argv[1]](fk)
+    {"launches": launches, "pages": pages}[sys.argv[1]](fk)
     print("done")
