@@ -201,6 +201,25 @@ __device__ __forceinline__ void class_range(int c, int s, u64 &lo, u64 &hi) {
   hi = (u64)(9 + f) << sh;
 }
 
+// f x rounded down, and up where UP, for 0 <= f <= 1: f is a 24-bit integer
+// times a power of two, the product fits 128 bits.  (A float64 product drops up to
+// ten bits of a sum, and a border that it moves is another token.)
+template <bool UP> __device__ __forceinline__ u64 times(float f, u64 x) {
+  const unsigned b = __float_as_uint(f), e = b >> 23;
+  const u64 m = (b & 0x7fffff) | (e ? 0x800000u : 0u);
+  const int sh = 150 - (int)max(e, 1u);  // f = m 2^-sh, 23 <= sh <= 149
+  const u64 hi = __umul64hi(m, x), lo = m * x;
+  u64 q = 0, rest = hi | lo;
+  if (sh < 64) {
+    q = hi << (64 - sh) | lo >> sh;
+    rest = lo << (64 - sh);
+  } else if (sh < 88) {  // (the product is below 2^87)
+    q = hi >> (sh - 64);
+    rest = (hi & ((1ull << (sh - 64)) - 1)) | lo;
+  }
+  return q + (UP && rest != 0);
+}
+
 // Inclusive running sum over the wave's lanes (all of them active) without
 // LDS: shifts within each row of 16, then the rows' sums handed on.
 __device__ __forceinline__ u64 wave_scan64(u64 v) {
@@ -553,11 +572,7 @@ __global__ __launch_bounds__(256) void k_sample_cut(Args a) {
   }
   const float top_p = r.top_p;
   if (top_p < 1.f) {
-    auto reach = [&](u64 w) {
-      const u64 x = (u64)ceil((double)top_p * (double)w);
-      return x < 1 ? 1 : x > w ? w : x;
-    };
-    const u64 nl = reach(wl), nh = reach(wh);
+    const u64 nl = times<true>(top_p, wl), nh = times<true>(top_p, wh);
     if (ms[t] >= nl && m0 < nl) pl_s = t;
     if (ms[t] >= nh && m0 < nh) ph_s = t;
   }
@@ -854,8 +869,7 @@ __global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
       }
     }
     if (r.top_p < 1.f) {
-      u64 need = (u64)ceil((double)r.top_p * (double)total);
-      need = need < 1 ? 1 : need > total ? total : need;
+      const u64 need = times<true>(r.top_p, total);
       int c = r.pl;
       while (c < r.ph && upto[c] < need) ++c;
       class_range(c, a.s, lo, hi);
@@ -915,8 +929,7 @@ __global__ __launch_bounds__(kFinal) void k_sample_final(Args a) {
     return;
   }
   incl += before;
-  u64 target = (u64)((double)r.u * (double)total);
-  if (target >= total) target = total - 1;
+  const u64 target = times<false>(r.u, total);  // (u < 1: below total)
   if (target < incl && target >= incl - m) {
     sh.bin = t;
     sh.sum = incl - m;
