@@ -1368,7 +1368,7 @@ dbt_status decode_step_impl(dbt_model *m, dbt_kv *kv, const dbt_step_in *in, int
 // What a tree's attention costs beside its pages (schedule_tree), in pages of
 // reading time (8 KB of keys and values; 0.4 us for a workgroup while all read):
 // a piece's start, the merge's launch, and kTreeMergeRows rows' partial results
-// written and read.
+// written and read.  kTreePieces: see schedule_tree.
 constexpr int kTreeStart = 14, kTreeMerge = 14, kTreeMergeRows = 8, kTreePieces = 16;
 
 // may_be_empty: calls without a launch over the nodes
@@ -1447,13 +1447,15 @@ TreeLayout tree_layout(const dbt_config &c, int nodes) {
 
 // The schedule of up to kTreeSeqs sequences (see TreeSeqs): whole units, equal
 // runs for one round of workgroups, or units cut each by itself, whichever the
-// estimate makes shortest.  Measured (us; whole, runs, each by itself):
-//   8 KV heads, one sequence of 777, 96 rows         24.7  17.0  17.0
-//   one KV head, 13 of 150-4096, 32 rows             45.3  25.0  20.8
-//   8 KV heads, 8 of 16k-32k, 256 rows              694.5 285.5 289.7
-//   4 KV heads, 16 of 300-1500, 1024 rows            55.1  85.0  68.4
+// estimate makes shortest.  Measured (us a call by events; whole, runs, each by itself):
+//   8 KV heads, one sequence of 777, 96 rows         24.6  17.1  17.5
+//   one KV head, 13 of 150-4096, 32 rows             68.0  22.8  20.2
+//   8 KV heads, 8 of 16k-32k, 256 rows              688.6 278.8 284.3
+//   4 KV heads, 16 of 300-1500, 1024 rows            53.1  81.4  66.8
+//   8 KV heads, 32 of 4096, 64 rows                  97.9 107.9 103.1
+// (in the last line the estimate takes the third, 5 % from the best.)
 // Whole units go longest first; where one round takes them all, long and short in
-// turns, which fall to one XCD and one compute unit together (the last line; 60 in
+// turns, which fall to one XCD and one compute unit together (the fourth line; 60 in
 // the sequences' order).
 void schedule_tree(const dbt_config &c, int block, int blocks, TreeSeqs *g) {
   long long total = 0;
@@ -1467,7 +1469,8 @@ void schedule_tree(const dbt_config &c, int block, int blocks, TreeSeqs *g) {
     longest = std::max(longest, stages(i));
   }
   const long long units = (long long)g->n * c.n_kv_heads, W = std::max(1, kTreeWorkgroups / blocks);
-  // (a unit in at most kTreePieces pieces: the merge reads eight at a time)
+  // (a unit in at most kTreePieces pieces, or one more where runs go over units'
+  // ends: the merge reads eight at a time)
   const long long rounds = (units + W - 1) / W, P = kTreeStagePages,
                   run = std::max<long long>((total + W - 1) / W, (longest + kTreePieces - 1) / kTreePieces);
   long long part = longest;  // least run for which the units, each cut by itself, fit

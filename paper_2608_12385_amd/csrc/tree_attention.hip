@@ -96,8 +96,7 @@ __device__ __forceinline__ Piece piece_at(const TreeAttn &a, int s, int end) {
 // Workgroups are dealt to the eight XCDs in turn: workgroup b takes a place that
 // keeps neighbours on one XCD.  Those are the blocks of one run, which read the
 // same pages at the same time: all but the first of them from the XCD's L2
-// (8 x 16k-32k positions, two blocks: 0.8 GB from memory; with each block's runs cut
-// where they come, so that the two meet at other times, 1.6 GB).
+// (8 x 16k-32k positions, two blocks: counters show 0.90 GB read, the cache is 0.83).
 __device__ __forceinline__ int schedule_place(int b, int n) {
   const int x = b & 7, q = n >> 3, r = n & 7;
   return x * q + min(x, r) + (b >> 3);
@@ -122,20 +121,22 @@ constexpr float kLazyMargin = 8.f;
 // position `base` on; those pairs take a masked path.
 //
 // Up to 64 rows RT is 1, so that all four SIMDs have a part of them, and one
-// workgroup alone reads each page: the loads' non-temporal hint takes 97 us to 90
-// with 8 rows (32 x 4096 positions, eight KV heads) and 111 to 104 with 64.  More
-// rows are faster with two tiles a wave, whose softmax steps run side by side and
-// which read LDS half as often; the hint gains nothing there, and where several blocks
-// share the pages in an L2 it costs 2-5 %.  Without the hint 8 and 64 rows take 100
-// and 115 us with RT = 2, which leaves two SIMDs idle; eight waves that also share a
-// stage's pairs (merged at the end) take 107 for the 64 rows but 142 against 111 for
-// 48 x 200-4000, since nothing runs while the compute unit's one workgroup begins
-// its next piece.
+// workgroup alone reads each page: the loads' non-temporal hint takes 97 us to 91
+// with 8 rows (32 x 4096 positions, eight KV heads), 112 to 103 with 64 and 109 to
+// 99 over 48 x 200-4000 (whole calls, the merge with them, by events).  With RT = 2,
+// which leaves two SIMDs idle, the three take 100, 112 and 115.  More rows are faster
+// with two tiles a wave, whose softmax steps run side by side and which read LDS half
+// as often; the hint gains nothing there (8 x 16k-32k with 128 rows: 176 and 178), and
+// where several blocks share the pages in an L2 it costs 2-5 % (256 rows: 285 against
+// 280, 16 x 300-1500 with 1024 rows 56 against 54).  Eight waves that also share a
+// stage's pairs (merged at the end) took 107 against 111 for the 64 rows, both without
+// the hint, but 142 against 111 for 48 x 200-4000, since nothing runs while the compute
+// unit's one workgroup begins its next piece.
 //
-// Bound: up to 64 rows the memory (90 us: 6.1 TB/s).  From 128 rows the matrix
-// unit beside the softmax: 16 x 300-1500 with 1024 rows 54 us, 3.1e10 operations
-// (the longest sequence alone takes 45); 8 x 16k-32k with 256 rows 285 us, 2.1e11
-// operations, 215 without the loads and 171 without the multiplies.
+// Bound: up to 64 rows the memory (32 x 4096 with 64 rows: 0.54 GB read in 94 us of
+// the kernel, 5.8 TB/s).  From 128 rows the matrix unit beside the softmax, whose
+// steps for a pair follow each other: 16 x 300-1500 with 1024 rows 54 us for 3.1e10
+// operations, 8 x 16k-32k with 256 rows 280 us for 2.1e11.
 template <int RT, typename QT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_tree_attn_bf16(TreeAttn a) {
   constexpr int DH = 128, NW = 4, SP = 4, PB = 16 * DH;  // waves; pages of a stage; elements of a page
