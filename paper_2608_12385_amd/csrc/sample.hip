@@ -19,14 +19,15 @@
 //
 // Six kernels, for 64 rows of 128256 tokens with one branch and requests of every
 // kind: statistics of the tiles 20 us, row constants 9 (without branches the
-// weights' kernel finds the maximum itself), weights and histograms 32, cut
-// classes 7, list 6, cut and draw 23 (a call whose rows have no cut skips the list
-// and the cut classes); 500 rows of 50257 without branches: 16-20, none, 41, 6, 17, 20.
-// The floor is the logits read once, 13 and 20 us.  The weights are
-// bound by vector instructions, some 44 a token of which half are float64 (28 of
-// the 41 us); the statistics by memory without branches and by the exponentials
+// weights' kernel finds the maximum itself), weights and histograms 33, cut
+// classes 7, list 6, cut and draw 21 (a call whose rows have no cut skips the list
+// and the cut classes); 500 rows of 50257 without branches: 16, none, 43, 6, 17, 20.
+// The floor is the logits read once, 13 and 20 us; the kernels read them twice.  The
+// weights are bound by vector instructions, some 44 a token of which half are float64;
+// the statistics by memory without branches and by the exponentials
 // with one; the list by the lines of logits around its tokens; the row kernels by
-// their chains of dependent steps, a workgroup a row.
+// their chains of dependent steps, a workgroup a row (64 rows leave three quarters
+// of the compute units idle, and a flat row's candidate tiles are all its workgroup's).
 #include <cmath>
 
 #include "../../include/dbt.h"
